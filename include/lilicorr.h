@@ -41,6 +41,7 @@ extern "C" {
 typedef enum {
     LILICORR_F32 = 0,  /* IEEE binary32 */
     LILICORR_BF16 = 1, /* bfloat16 bit patterns (uint16) */
+    LILICORR_F16 = 2,  /* IEEE binary16; only the paged-cache calls take it */
 } lilicorr_dtype;
 
 typedef enum {
@@ -465,6 +466,140 @@ size_t lilicorr_scorer_workspace_bytes(int64_t N, int64_t S, int K, int H, int F
 lilicorr_status lilicorr_scorer_forward(float *X, int64_t N, int64_t S, int K, int H, int heads,
                                         int F, int layers, const void *packed, void *workspace,
                                         size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Paged cache — what a serving program runs around the draft path. The target that checks a drafted
+ * block, and the drafter itself (its block attends to the context and to itself, Sec. 3.1), read the
+ * keys and values of every request's tokens from a cache kept in pages, so that requests of any
+ * length share one pool. Four calls: lilicorr_page_plan gives every new token of a step its place,
+ * lilicorr_qk_norm_rope norms and rotates queries and keys and fills those places,
+ * lilicorr_window_attention and lilicorr_prefix_attention read them.
+ *
+ * Lengths, tables and slots live on the device and are made there, so that a step needs no host
+ * synchronisation. A wrong index there costs no memory safety: a page outside [0, pages) is a page
+ * that is not there, and everything else is clamped. Index arrays need only their type's alignment
+ * (LILICORR_ERR_ALIGNMENT otherwise), everything else 16 bytes.
+ */
+
+/*
+ * Places for one step's tokens. Request n holds lengths[n] tokens and brings incoming[n] new ones;
+ * incoming[n] < 0 ends it. P = page_size, M = table_width, C = queue_size.
+ *   lengths, incoming [N] int32.
+ *   pages      [N][2] int32: entries of the request's table row filled so far (end), and the first
+ *              entry that the window has not given back yet (since; 0 at the start).
+ *   table      [N][M] int32, in place: page of tokens e P .. e P + P - 1 of request n at [n][e].
+ *   queue      [C] int32, in place: a ring of free pages, cursor [3] int64 its head, its tail (both
+ *              only grow; entries head .. tail - 1, mod C, are free) and a third value, not read.
+ *              C at least the number of pages there are.
+ *   window     0, or W >= 1: no later query sees a key more than W - 1 before it, save the first
+ *   sinks      S tokens (0 without a window), so pages wholly behind lengths[n] - W + 1 and past the
+ *              first ceil(S / P) go back to the queue. Their table entries keep their value.
+ * A request needs ceil((lengths + incoming) / P) entries, M at most; the ones it lacks are taken from
+ * the queue's head, requests in order. Where the queue runs out, an entry gets -1 and is asked for
+ * again by the next call. An ended request gives back every page it holds: its row's first
+ * min(ceil(S/P), end) entries and then entries since .. end - 1.
+ *   pages_out  [N][2] int32, cursor_out [3] int64 (the third: pages that were lacking): for the next
+ *              call. They must not overlap the inputs: workgroups read those while others write.
+ *   starts     [N + 1] int32: tokens of the requests before n (prefix sums of max(incoming, 0),
+ *              at most `tokens`); totals [N] int32: lengths + incoming (0 for an ended request).
+ *   slots      [tokens] int32: page * P + position % P of each new token, request by request, -1
+ *              where it has no page; positions [tokens] int32. Past starts[N] both are -1.
+ * Drafts that were rejected need nothing: call with the shorter length, the pages stay.
+ * Limits: 1 <= N <= 4096, 1 <= P <= 65536, P * M < 2^31, 0 <= tokens < 2^31, C < 2^31.
+ */
+lilicorr_status lilicorr_page_plan(const int32_t *lengths, const int32_t *incoming,
+                                   const int32_t *pages, int32_t *table, int32_t *queue,
+                                   const int64_t *cursor, int64_t N, int page_size,
+                                   int64_t table_width, int64_t queue_size, int64_t tokens,
+                                   int64_t window, int64_t sinks, int32_t *pages_out,
+                                   int64_t *cursor_out, int32_t *starts, int32_t *totals,
+                                   int32_t *slots, int32_t *positions, hipStream_t stream);
+
+/* The cache: element x of head h of the token at place o of page p lies at
+ * p * page_stride + o * token_stride + h * head_stride + x of k (keys) and of v (values). Strides are
+ * in elements and multiples of 8, so [pages][page_size][heads][d], [pages][heads][page_size][d] and
+ * keys and values side by side in one buffer all fit. */
+typedef struct {
+    void *k, *v;          /* elements of `dtype` */
+    lilicorr_dtype dtype; /* LILICORR_BF16 or LILICORR_F16 */
+    int page_size;
+    int heads;            /* key heads */
+    int d;                /* head width: a multiple of 8 with 16 <= d <= 256 */
+    int64_t pages;
+    int64_t page_stride, token_stride, head_stride;
+} lilicorr_cache;
+
+/*
+ * Head norms, rotation and cache write in one pass. For every token t and every head of q and k:
+ *   y = x / sqrt(mean(x^2) + eps) * weight   (weight NULL: y = x)
+ *   then, with c, s the row cos_sin[positions[t]], the pair (a, b) number i of the first `rot`
+ *   elements becomes (a c_i - b s_i, a s_i + b c_i); pairs are elements (i, i + rot / 2), or
+ *   (2 i, 2 i + 1) when `interleaved`.
+ * All of it in fp32 from the stored values, rounded once (nearest, ties to even) at the end. q goes to
+ * q_out, k and (as it is) v to the cache at slots[t]; a token with slots[t] outside the cache
+ * (-1: no page) is not written there. A position outside [0, max_positions) gives zeros in q_out and
+ * no cache write (the rows past the last token of lilicorr_page_plan).
+ *   q [tokens][heads][d], k, v [tokens][cache heads][d] of the cache's dtype; q_stride, k_stride,
+ *   v_stride elements from token to token (multiples of 8: views of one projection's output fit).
+ *   q_weight, k_weight [d] fp32 or NULL; cos_sin [max_positions][rot] fp32, rot / 2 cosines and then
+ *   rot / 2 sines a row.
+ *   q_out [tokens][heads][d], contiguous; it may be q itself.
+ * Two tokens of a call must not have the same slot. Limits: rot a multiple of 16, 0 <= rot <= d
+ * (cos_sin may be NULL when 0); tokens < 2^31.
+ */
+lilicorr_status lilicorr_qk_norm_rope(const void *q, int64_t q_stride, int heads, const void *k,
+                                      int64_t k_stride, const void *v, int64_t v_stride,
+                                      int64_t tokens, const int32_t *slots,
+                                      const int32_t *positions, const float *cos_sin,
+                                      int64_t max_positions, int rot, int interleaved,
+                                      const float *q_weight, const float *k_weight, float eps,
+                                      const lilicorr_cache *cache, void *q_out,
+                                      hipStream_t stream);
+
+/*
+ * Attention over the paged cache. Request n has T = starts[n+1] - starts[n] queries (rows starts[n] ..
+ * of q), at positions totals[n] - T .. totals[n] - 1, and totals[n] keys, the queries' own among them:
+ *   out[t][h] = sum_j softmax_j(scale q[t][h] . k[j][h / (heads / cache heads)]) v[j][..]
+ * over the keys j < totals[n] that the query at position p sees: j <= p when `causal`, and
+ * j > p - window or j < sinks when window > 0, on pages that the table lists. A query that sees none
+ * gives zeros; a key that it does not see has no effect on it, whatever its key and value hold.
+ *   shared_table, shared_length   lilicorr_prefix_attention only: the first shared_length tokens of
+ *       every request are the ones on these pages (ceil(shared_length / page_size) entries). Every
+ *       query sees all of them; table, totals and positions count from there on, window must be 0.
+ *       They are read once for all queries of a key head instead of once for each request.
+ * Scores, softmax and sums in fp32; probabilities are rounded to the cache's type for the second
+ * product, and the output once more. The result does not depend on what else runs, and is the same
+ * on every call with the same arguments.
+ *   max_tokens, max_length   upper bounds of T and totals that the host knows (they choose tiles and
+ *       how far the key axis is split). Queries and keys past them are not computed or seen.
+ *   workspace   device scratch of the size the query gives, caller-owned, zero-filled once before its
+ *       first use; every call leaves it ready for the next. Calls sharing it must not overlap.
+ * Limits: heads a multiple of cache heads; tokens * heads < 2^31; page_size * table_width < 2^31;
+ * N < 2^24; scale > 0 and finite. out must not overlap q.
+ */
+typedef struct {
+    const void *q;                  /* [tokens][heads][d] of the cache's dtype */
+    void *out;                      /* [tokens][heads][d], contiguous */
+    lilicorr_cache cache;
+    const int32_t *table;           /* [N][table_width] */
+    const int32_t *starts, *totals; /* [N + 1], [N] */
+    const int32_t *shared_table;    /* lilicorr_prefix_attention */
+    void *workspace;
+    size_t workspace_bytes;
+    int64_t tokens, q_stride;       /* q_stride: elements from token to token, a multiple of 8 */
+    int64_t N, table_width;
+    int64_t shared_length;
+    int64_t window, sinks;
+    int64_t max_tokens, max_length;
+    int heads, causal;
+    float scale;
+} lilicorr_attention_args;
+
+/* Workspace bytes of the call (pointers are not looked at); 0 if the sizes are unsupported. */
+size_t lilicorr_window_attention_workspace_bytes(const lilicorr_attention_args *args);
+size_t lilicorr_prefix_attention_workspace_bytes(const lilicorr_attention_args *args);
+lilicorr_status lilicorr_window_attention(const lilicorr_attention_args *args, hipStream_t stream);
+lilicorr_status lilicorr_prefix_attention(const lilicorr_attention_args *args, hipStream_t stream);
 
 /* Static, human-readable name of a status code. */
 const char *lilicorr_status_string(lilicorr_status s);

@@ -17,6 +17,13 @@ The four steps run in hand-written HIP kernels behind a C ABI (include/lilicorr.
   lilicorr_block_graph_*      top-K + one fused pass recorded as one HIP graph, replayed per block
   lilicorr_scorer_*           scoring-Transformer stand-in over the candidate lattice (cost only)
 
+Around the path, over a paged cache (paged.py):
+
+  lilicorr_page_plan          lengths -> page tables, slots, positions   (one step's places)
+  lilicorr_qk_norm_rope       head norms, rotation, keys and values into the cache
+  lilicorr_window_attention   paged attention with a sliding window and visible first tokens
+  lilicorr_prefix_attention   paged attention of a batch that shares a long prefix
+
 This module only marshals arguments: torch supplies device memory and the current HIP stream,
 and every step of the path runs in the library's kernels. There is no fallback: if the library
 is missing or fails to load, every call raises.
@@ -134,6 +141,7 @@ def load_library() -> ctypes.CDLL:
         "lilicorr_scorer_forward": ([P, I64, I64, I, I, I, I, I, P, P, SZ, P], I),
         "lilicorr_status_string": ([I], ctypes.c_char_p),
     }
+    sig.update(paged.SIGNATURES)
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -802,3 +810,9 @@ def scorer_forward(X: torch.Tensor, packed: torch.Tensor, S: int, K: int, heads:
     lilicorr_scorer_forward(_dev(X, "X", (torch.float32,)), N, S, K, H, heads, F, layers,
                             _dev(packed, "packed"), _dev(ws, "workspace"), ws.numel(), _stream())
     return X
+
+
+from . import paged  # noqa: E402  (needs the names above)
+from .paged import *  # noqa: E402,F401,F403
+
+__all__ += paged.__all__

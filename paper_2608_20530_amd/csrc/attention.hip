@@ -1,0 +1,226 @@
+// lilicorr_window_attention and lilicorr_prefix_attention: checks, tiles and chunks, launches.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "attention.hpp"
+#include "common.hpp"
+#include "lilicorr.h"
+#include "paged.hpp"
+
+namespace lilicorr {
+namespace {
+
+constexpr size_t kHeaderBytes = 256;
+constexpr int kTargetItems = 512;  // workgroups that fill the chip: two on each of 256 compute units
+
+// One pass over keys: which tile height, how many tiles and chunks
+struct Pass {
+  int BM, tiles, chunk, chunks;
+};
+
+struct Plan {
+  bool shared;
+  Pass first, tail;  // the shared keys' pass and the requests' own
+  int slots;
+  int64_t rows;
+  size_t bytes;
+};
+
+int tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+
+// keys: the most that a tile sees; stage: the largest stage of the kernels, which chunks are whole
+// multiples of
+Pass make_pass(int64_t rows_each, int64_t tiles, int heads, int64_t keys, int BM) {
+  Pass p;
+  p.BM = BM;
+  p.tiles = (int)tiles;
+  constexpr int64_t kLeast = 256;  // keys of a chunk that are worth its partial results
+  const int64_t items = tiles * heads;
+  int64_t chunks = (kTargetItems + items - 1) / items;
+  const int64_t most = (keys + kLeast - 1) / kLeast;
+  if (chunks > most) chunks = most;
+  if (chunks < 1) chunks = 1;
+  int64_t chunk = (keys + chunks - 1) / chunks;
+  chunk = (chunk + 127) / 128 * 128;
+  if (chunk < 128) chunk = 128;
+  p.chunk = (int)chunk;
+  p.chunks = (int)((keys + chunk - 1) / chunk);
+  if (p.chunks < 1) p.chunks = 1;
+  return p;
+}
+
+lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p) {
+  if (const lilicorr_status s = cache_sizes(a.cache)) return s;
+  if (a.tokens < 0 || a.N < 1 || a.table_width < 1 || a.heads < 1 || a.window < 0 || a.sinks < 0 ||
+      a.max_tokens < 0 || a.max_length < 0 || a.q_stride < 0)
+    return LILICORR_ERR_INVALID_ARG;
+  if (a.heads % a.cache.heads) return LILICORR_ERR_INVALID_ARG;
+  if (!(a.scale > 0.f) || !isfinite(a.scale)) return LILICORR_ERR_INVALID_ARG;
+  if (a.sinks > 0 && a.window == 0) return LILICORR_ERR_INVALID_ARG;
+  if (shared ? (a.shared_length < 1 || a.window != 0) : a.shared_length != 0)
+    return LILICORR_ERR_INVALID_ARG;
+  constexpr int64_t kMost = (int64_t)1 << 30;
+  if (a.heads > 65535 || a.N > (1 << 20) || a.tokens > kMost / a.heads ||
+      a.table_width > kMost / a.cache.page_size || a.shared_length > kMost)
+    return LILICORR_ERR_UNSUPPORTED;
+  if (!stride_ok(a.q_stride)) return LILICORR_ERR_ALIGNMENT;
+
+  const int64_t group = a.heads / a.cache.heads;
+  const int64_t max_tokens = a.max_tokens < a.tokens ? a.max_tokens : a.tokens;
+  p.shared = shared;
+  p.rows = a.tokens * a.heads;
+  const int64_t own = max_tokens * group;
+  const int BM = tile_rows(own);
+  const int64_t tiles = own <= BM ? a.N : a.tokens * group / BM + a.N;
+  int64_t keys = a.table_width * a.cache.page_size;
+  if (a.max_length < keys) keys = a.max_length;
+  if (a.window) {
+    // a tile's queries see at most this many: from the first one's window to the last one itself, or
+    // to the request's last token
+    const int64_t tile_tokens = BM / group + 1;
+    const int64_t seen = a.window + a.sinks +
+                         (a.causal && tile_tokens < max_tokens ? tile_tokens : max_tokens);
+    if (seen < keys) keys = seen;
+  }
+  p.tail = make_pass(own, tiles, a.cache.heads, keys, BM);
+  p.slots = p.tail.chunks;
+  if (shared) {
+    const int64_t all = a.tokens * group;
+    const int BS = tile_rows(all);
+    p.first = make_pass(all, (all + BS - 1) / BS, a.cache.heads, a.shared_length, BS);
+    p.slots += p.first.chunks;
+  }
+  const int64_t most_items = 0x7fffffffll / a.cache.heads;
+  if ((int64_t)p.tail.tiles * p.tail.chunks > most_items ||
+      (shared && (int64_t)p.first.tiles * p.first.chunks > most_items))
+    return LILICORR_ERR_UNSUPPORTED;
+  p.bytes = kHeaderBytes;
+  if (p.slots > 1) p.bytes += (size_t)p.slots * p.rows * (8 + (size_t)a.cache.d * 4);
+  return LILICORR_OK;
+}
+
+template <typename C>
+void launch(const AttnArgs& a, int chunks, hipStream_t stream) {
+  static const hipError_t attr =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(attention_kernel<C>),
+                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::kLds);
+  (void)attr;
+  hipLaunchKernelGGL(attention_kernel<C>, dim3((unsigned)((int64_t)a.tiles * chunks * a.kv_heads)),
+                     dim3(C::kThreads), C::kLds, stream, a);
+}
+
+template <typename T>
+void launch_pass(AttnArgs a, const Pass& p, hipStream_t stream) {
+  a.tiles = p.tiles;
+  a.chunk = p.chunk;
+  if (a.d <= 64) {
+    if (p.BM == 32) launch<AttnConfig<T, 64, 1, 4, 1>>(a, p.chunks, stream);
+    else if (p.BM == 64) launch<AttnConfig<T, 64, 2, 2, 1>>(a, p.chunks, stream);
+    else launch<AttnConfig<T, 64, 4, 1, 2>>(a, p.chunks, stream);
+  } else if (a.d <= 128) {
+    if (p.BM == 32) launch<AttnConfig<T, 128, 1, 4, 1>>(a, p.chunks, stream);
+    else if (p.BM == 64) launch<AttnConfig<T, 128, 2, 2, 1>>(a, p.chunks, stream);
+    else launch<AttnConfig<T, 128, 4, 1, 2>>(a, p.chunks, stream);
+  } else {
+    if (p.BM == 32) launch<AttnConfig<T, 256, 1, 2, 1>>(a, p.chunks, stream);
+    else if (p.BM == 64) launch<AttnConfig<T, 256, 2, 2, 1>>(a, p.chunks, stream);
+    else launch<AttnConfig<T, 256, 4, 1, 1>>(a, p.chunks, stream);
+  }
+}
+
+template <typename T>
+lilicorr_status run(const lilicorr_attention_args& x, const Plan& p, hipStream_t stream) {
+  AttnArgs a = {};
+  const lilicorr_cache& c = x.cache;
+  a.q = (const uint16_t*)x.q; a.k = (const uint16_t*)c.k; a.v = (const uint16_t*)c.v;
+  a.out = (uint16_t*)x.out;
+  a.table = x.table; a.starts = x.starts; a.totals = x.totals;
+  a.q_stride = x.q_stride; a.page_stride = c.page_stride; a.token_stride = c.token_stride;
+  a.head_stride = c.head_stride;
+  a.rows = p.rows;
+  a.N = (int)x.N; a.table_width = (int)x.table_width; a.pages = (int)c.pages; a.page_size = c.page_size;
+  // n / P = (n * mul) >> shift for n < 2^31, mul = floor(2^shift / P) + 1 below 2^32
+  int bits = 0;
+  while ((1 << bits) < c.page_size) ++bits;
+  a.page_shift = 31 + bits;
+  a.page_mul = (uint32_t)((((uint64_t)1 << a.page_shift) / c.page_size) + 1);
+  a.tokens = (int)x.tokens; a.heads = x.heads; a.kv_heads = c.heads; a.group = x.heads / c.heads;
+  a.d = c.d;
+  a.window = (int)(x.window < (1 << 30) ? x.window : (1 << 30));
+  a.sinks = (int)(x.sinks < (1 << 30) ? x.sinks : (1 << 30));
+  a.causal = x.causal != 0;
+  a.max_tokens = (int)(x.max_tokens < x.tokens ? x.max_tokens : x.tokens);
+  a.max_length = (int)(x.max_length < (1 << 30) ? x.max_length : (1 << 30));
+  a.split = p.slots > 1;
+  a.scale2 = x.scale * 1.4426950408889634f;
+  if (a.split) {
+    unsigned char* w = (unsigned char*)x.workspace + kHeaderBytes;
+    a.part_o = (float*)w;
+    a.part_ml = (f32x2_t*)(w + (size_t)p.slots * p.rows * c.d * 4);
+  }
+  if (p.shared) {
+    AttnArgs s = a;
+    s.shared = (int)x.shared_length;
+    s.table = x.shared_table;
+    s.table_width = (int)((x.shared_length + c.page_size - 1) / c.page_size);
+    s.max_length = s.shared;
+    s.max_tokens = a.tokens;
+    s.causal = s.window = s.sinks = 0;
+    launch_pass<T>(s, p.first, stream);
+    a.slot0 = p.first.chunks;
+  }
+  launch_pass<T>(a, p.tail, stream);
+  if (a.split) {
+    int lanes = 4;
+    while (lanes * 4 < c.d) lanes *= 2;
+    const int64_t per = kJoinThreads / lanes;
+    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((p.rows + per - 1) / per)),
+                       dim3(kJoinThreads), 0, stream, a.part_o, a.part_ml, p.rows, p.slots, c.d,
+                       lanes, a.starts, a.N, a.heads, a.out);
+  }
+  return launch_status();
+}
+
+size_t workspace_bytes(const lilicorr_attention_args* a, bool shared) {
+  Plan p;
+  return a && make_plan(*a, shared, p) == LILICORR_OK ? p.bytes : 0;
+}
+
+lilicorr_status attention(const lilicorr_attention_args* a, bool shared, hipStream_t stream) {
+  if (!a) return LILICORR_ERR_INVALID_ARG;
+  Plan p;
+  if (const lilicorr_status s = make_plan(*a, shared, p)) return s;
+  if (a->tokens == 0) return LILICORR_OK;
+  if (!a->q || !a->out || !a->cache.k || !a->cache.v || !a->table || !a->starts || !a->totals)
+    return LILICORR_ERR_INVALID_ARG;
+  if (shared != (a->shared_table != nullptr) || a->q == a->out) return LILICORR_ERR_INVALID_ARG;
+  if (!aligned16(a->q) || !aligned16(a->out) || !aligned16(a->cache.k) || !aligned16(a->cache.v) ||
+      !aligned16(a->workspace) || !aligned4(a->table) || !aligned4(a->starts) ||
+      !aligned4(a->totals) || !aligned4(a->shared_table))
+    return LILICORR_ERR_ALIGNMENT;
+  if (!a->workspace || a->workspace_bytes < p.bytes) return LILICORR_ERR_WORKSPACE;
+  if (a->max_tokens == 0) return LILICORR_OK;
+  return a->cache.dtype == LILICORR_BF16 ? run<Bf16>(*a, p, stream) : run<F16>(*a, p, stream);
+}
+
+}  // namespace
+}  // namespace lilicorr
+
+extern "C" size_t lilicorr_window_attention_workspace_bytes(const lilicorr_attention_args* args) {
+  return lilicorr::workspace_bytes(args, false);
+}
+
+extern "C" size_t lilicorr_prefix_attention_workspace_bytes(const lilicorr_attention_args* args) {
+  return lilicorr::workspace_bytes(args, true);
+}
+
+extern "C" lilicorr_status lilicorr_window_attention(const lilicorr_attention_args* args,
+                                                     hipStream_t stream) {
+  return lilicorr::attention(args, false, stream);
+}
+
+extern "C" lilicorr_status lilicorr_prefix_attention(const lilicorr_attention_args* args,
+                                                     hipStream_t stream) {
+  return lilicorr::attention(args, true, stream);
+}

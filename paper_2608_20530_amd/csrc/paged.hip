@@ -1,0 +1,481 @@
+// The paged cache's bookkeeping and its writer: lilicorr_page_plan (places for one step's tokens) and
+// lilicorr_qk_norm_rope (head norms, rotation and cache write in one pass).
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "common.hpp"
+#include "lilicorr.h"
+#include "paged.hpp"
+
+namespace lilicorr {
+namespace {
+
+// ---- page plan ---------------------------------------------------------------------------------
+// Everything a request needs follows from four prefix sums over the requests before it: new tokens,
+// pages taken, pages given back (and the head of the queue). The requests are few (a step's batch),
+// so every workgroup makes the sums for itself, 16 bytes a request from the L2, and takes its share
+// of the items: tokens, then taken pages, then given-back pages, each found by a binary search in the
+// sums. No workgroup waits for another and one launch does it all. Nothing that is read is written in
+// the same call: entries [end, end + take) of a table row and ring places from the tail on are
+// written, entries below end and places from the head on are read. Bound by latency: one round trip
+// for the lengths, the sums in LDS, a search of log2 N LDS reads, one round trip for the page.
+constexpr int kPlanThreads = 256;
+constexpr int kPlanMaxN = 4096;
+
+struct PlanArgs {
+  const int32_t *lengths, *incoming, *pages;
+  int32_t *table, *queue;
+  const int64_t* cursor;
+  int N, P, M, C;
+  int64_t tokens, window;
+  int first;  // table entries that hold the first `sinks` tokens
+  int32_t* pages_out;
+  int64_t* cursor_out;
+  int32_t *starts, *totals, *slots, *positions;
+};
+
+struct PlanRow {
+  int64_t total;
+  int fresh, take, give, end, since, kept;
+  bool ended;
+};
+
+__device__ __forceinline__ PlanRow plan_row(const PlanArgs& a, int n) {
+  PlanRow r;
+  const int L = max(a.lengths[n], 0), I = a.incoming[n];
+  r.end = min(max(a.pages[2 * n], 0), a.M);
+  r.since = max(max(a.pages[2 * n + 1], 0), a.first);
+  r.kept = min(a.first, r.end);
+  r.ended = I < 0;
+  if (r.ended) {
+    r.fresh = r.take = 0;
+    r.total = 0;
+    r.give = r.kept + max(r.end - r.since, 0);
+  } else {
+    r.fresh = I;
+    r.total = (int64_t)L + I;
+    const int64_t need = (r.total + a.P - 1) / a.P;
+    r.take = max((int)(need < a.M ? need : a.M) - r.end, 0);
+    int upto = 0;
+    if (a.window) {
+      const int64_t behind = (int64_t)L - a.window + 1;  // tokens that no query sees any more
+      if (behind > 0) upto = (int)(behind / a.P < r.end ? behind / a.P : r.end);
+    }
+    r.give = max(upto - r.since, 0);
+  }
+  return r;
+}
+
+__device__ __forceinline__ int64_t wave_scan(int64_t v) {
+  const int lane = lane_id();
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) {
+    const int64_t o = (int64_t)shfl64((uint64_t)v, lane - m < 0 ? lane : lane - m);
+    if (lane >= m) v += o;
+  }
+  return v;
+}
+
+__device__ __forceinline__ int clamp32(int64_t v) {
+  return v < 0x7fffffff ? (int)v : 0x7fffffff;
+}
+
+// the last n in [0, N) with sums[n] <= at, for sums[0] = 0 and at < sums[N]
+__device__ __forceinline__ int find_row(const int* sums, int N, int at) {
+  int lo = 0, hi = N;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (sums[mid] <= at) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a) {
+  extern __shared__ int plan_smem[];
+  int* const s_tok = plan_smem;              // [N + 1] sums before each request
+  int* const s_take = s_tok + a.N + 1;
+  int* const s_give = s_take + a.N + 1;
+  __shared__ int64_t s_part[3][kPlanThreads / kWave];
+  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
+
+  const int64_t head = a.cursor[0], tail = a.cursor[1];
+  int64_t base[3] = {0, 0, 0};
+  for (int n0 = 0; n0 < a.N; n0 += kPlanThreads) {
+    const int n = n0 + tid;
+    PlanRow r = {};
+    if (n < a.N) r = plan_row(a, n);
+    int64_t v[3] = {r.fresh, r.take, r.give}, in[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      in[i] = wave_scan(v[i]);
+      if (lane == kWave - 1) s_part[i][wave] = in[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      int64_t before = base[i], all = 0;
+#pragma unroll
+      for (int w = 0; w < kPlanThreads / kWave; ++w) {
+        if (w < wave) before += s_part[i][w];
+        all += s_part[i][w];
+      }
+      if (n < a.N) plan_smem[i * (a.N + 1) + n] = clamp32(before + in[i] - v[i]);
+      base[i] += all;
+    }
+    __syncthreads();
+  }
+  if (tid < 3) plan_smem[tid * (a.N + 1) + a.N] = clamp32(base[tid]);
+  __syncthreads();
+
+  // free pages, and where the queue's head and tail lie in the ring
+  const int64_t free64 = tail - head;
+  const int avail = free64 < 0 ? 0 : (int)(free64 < a.C ? free64 : a.C);
+  const int at_head = (int)(((head % a.C) + a.C) % a.C), at_tail = (int)(((tail % a.C) + a.C) % a.C);
+  auto ring = [&](int at, int i) {  // i < C
+    const uint32_t x = (uint32_t)at + (uint32_t)i;
+    return (int)(x < (uint32_t)a.C ? x : x - (uint32_t)a.C);
+  };
+
+  if (blockIdx.x == 0) {
+    for (int n = tid; n < a.N; n += kPlanThreads) {
+      const PlanRow r = plan_row(a, n);
+      const int granted = max(min(r.take, avail - min(s_take[n], avail)), 0);
+      a.pages_out[2 * n] = r.ended ? 0 : r.end + granted;
+      a.pages_out[2 * n + 1] = r.ended ? 0 : r.since + r.give;
+      a.totals[n] = clamp32(r.total);
+    }
+    for (int n = tid; n <= a.N; n += kPlanThreads)
+      a.starts[n] = s_tok[n] < a.tokens ? s_tok[n] : (int)a.tokens;
+    if (tid == 0) {
+      a.cursor_out[0] = head + (base[1] < avail ? base[1] : avail);
+      a.cursor_out[1] = tail + base[2];
+      a.cursor_out[2] = base[1] > avail ? base[1] - avail : 0;
+    }
+  }
+
+  const int fresh = s_tok[a.N], take = s_take[a.N], give = min(s_give[a.N], a.C);
+  const int64_t items = a.tokens + take + give;
+  for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + tid; i < items;
+       i += (int64_t)gridDim.x * kPlanThreads) {
+    if (i < a.tokens) {  // a token's slot and position
+      int slot = -1, pos = -1;
+      if (i < fresh) {
+        const int n = find_row(s_tok, a.N, (int)i);
+        pos = clamp32((int64_t)max(a.lengths[n], 0) + ((int)i - s_tok[n]));
+        const int e = pos / a.P;
+        const int end = min(max(a.pages[2 * n], 0), a.M);
+        int page = -1;
+        if (e < end) {
+          page = a.table[(int64_t)n * a.M + e];
+        } else if (e < a.M) {
+          const int64_t g = (int64_t)s_take[n] + (e - end);
+          if (g < avail) page = a.queue[ring(at_head, (int)g)];
+        }
+        if (page >= 0) slot = clamp32((int64_t)page * a.P + pos % a.P);
+      }
+      a.slots[i] = slot;
+      a.positions[i] = pos;
+    } else if (i < a.tokens + take) {  // a taken page into its table row
+      const int g = (int)(i - a.tokens);
+      const int n = find_row(s_take, a.N, g);
+      const int e = min(max(a.pages[2 * n], 0), a.M) + (g - s_take[n]);
+      if (e < a.M) a.table[(int64_t)n * a.M + e] = g < avail ? a.queue[ring(at_head, g)] : -1;
+    } else {  // a page that goes back to the queue
+      const int g = (int)(i - a.tokens - take);
+      const int n = find_row(s_give, a.N, g);
+      const PlanRow r = plan_row(a, n);
+      const int k = g - s_give[n];
+      const int e = r.ended ? (k < r.kept ? k : r.since + k - r.kept) : r.since + k;
+      if (e < a.M) a.queue[ring(at_tail, g)] = a.table[(int64_t)n * a.M + e];
+    }
+  }
+}
+
+// ---- head norms, rotation, cache write ---------------------------------------------------------
+// A head is held by LPH lanes, eight elements (16 bytes) each, so a wave has 64 / LPH heads at once
+// and a load or store instruction moves whole heads. The wave stays with one token for all of its
+// share of heads: the token's cosines and sines, its slot and the norm weights stay in registers. A
+// lane needs its partner's elements of the pairs (i, i + rot / 2): rot is a multiple of 16, so the
+// partner holds them at the same place and four 32-bit shuffles bring them. Bound by HBM: each
+// element read once and written once.
+constexpr int kRopeThreads = 256;
+
+struct RopeArgs {
+  const uint16_t *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  int64_t tokens;
+  int parts;  // waves that share a token
+  int heads, kv_heads, d, rot, interleaved;
+  const int32_t *slots, *positions;
+  const float* cos_sin;
+  int64_t max_positions;
+  const float *q_weight, *k_weight;
+  float eps;
+  uint16_t *k_cache, *v_cache, *q_out;
+  int64_t pages, page_stride, token_stride, head_stride;
+  int page_size;
+};
+
+template <int LPH>
+__device__ __forceinline__ float head_sum(float v) {
+  auto dpp = [](float x, auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value,
+                                                      0xf, 0xf, false));
+  };
+  v += dpp(v, std::integral_constant<int, 0xB1>{});   // quad_perm 1,0,3,2
+  v += dpp(v, std::integral_constant<int, 0x4E>{});   // quad_perm 2,3,0,1
+  v += dpp(v, std::integral_constant<int, 0x141>{});  // row_half_mirror
+  if (LPH >= 16) v += dpp(v, std::integral_constant<int, 0x140>{});  // row_mirror
+  if (LPH >= 32) v += __shfl_xor(v, 16, kWave);
+  return v;
+}
+
+// one lane's part of a head: weights of its own elements and of its partner's, cosines and sines of
+// its pairs
+struct RopeLane {
+  float cs[8], sn[8];   // interleaved: four pairs, in [0, 4)
+  int partner;          // lane that holds the other halves of the pairs
+  bool turned, upper;   // whether this lane's elements turn; whether they are the pairs' b
+};
+
+template <typename T, int LPH>
+__device__ __forceinline__ u32x4_t norm_turn(const u32x4_t& w, bool norm, const float (&wt)[8],
+                                             const float (&wp)[8], const RopeLane& r, int d,
+                                             float eps, int rot, int interleaved) {
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2_t t = T::unpack(w[i]);
+    x[2 * i] = t[0];
+    x[2 * i + 1] = t[1];
+  }
+  float inv = 1.f;
+  if (norm) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+    s = head_sum<LPH>(s);
+    inv = 1.f / sqrtf(s / (float)d + eps);
+  }
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = norm ? x[i] * inv * wt[i] : x[i];
+  if (rot) {
+    if (interleaved) {
+      if (r.turned) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float a = y[2 * i], b = y[2 * i + 1];
+          y[2 * i] = a * r.cs[i] - b * r.sn[i];
+          y[2 * i + 1] = a * r.sn[i] + b * r.cs[i];
+        }
+      }
+    } else {
+      u32x4_t o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = (uint32_t)__shfl((int)w[i], r.partner, kWave);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x2_t t = T::unpack(o[i]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int j = 2 * i + e;
+          const float z = norm ? t[e] * inv * wp[j] : t[e];
+          // a c - b s for the lower half, b c + a s for the upper one
+          const float turn = r.upper ? y[j] * r.cs[j] + z * r.sn[j] : y[j] * r.cs[j] - z * r.sn[j];
+          y[j] = r.turned ? turn : y[j];
+        }
+      }
+    }
+  }
+  u32x4_t out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = T::pack(y[2 * i], y[2 * i + 1]);
+  return out;
+}
+
+template <typename T, int LPH>
+__global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) {
+  constexpr int kHeads = kWave / LPH;  // heads a wave holds
+  const int lane = lane_id(), l = lane % LPH, g = lane / LPH;
+  const int e0 = l * 8;
+  const bool mine = e0 < a.d;  // lanes past the head's width hold nothing
+
+  RopeLane r;
+  const int half = a.rot / 2;
+  r.turned = mine && e0 < a.rot;
+  r.upper = e0 >= half;
+  const int po = a.interleaved || !r.turned ? e0 : (r.upper ? e0 - half : e0 + half);
+  r.partner = g * LPH + po / 8;
+  const bool norm_q = a.q_weight != nullptr, norm_k = a.k_weight != nullptr;
+  float qw[8], qp[8], kw[8], kp[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    qw[i] = norm_q && mine ? a.q_weight[e0 + i] : 1.f;
+    qp[i] = norm_q && mine ? a.q_weight[po + i] : 1.f;
+    kw[i] = norm_k && mine ? a.k_weight[e0 + i] : 1.f;
+    kp[i] = norm_k && mine ? a.k_weight[po + i] : 1.f;
+  }
+
+  const int qs = (a.heads + kHeads - 1) / kHeads, ks = (a.kv_heads + kHeads - 1) / kHeads;
+  const int steps = qs + 2 * ks;
+  const int64_t waves = (int64_t)gridDim.x * (kRopeThreads / kWave);
+  const int64_t items = a.tokens * a.parts;
+  for (int64_t it = (int64_t)blockIdx.x * (kRopeThreads / kWave) + threadIdx.x / kWave; it < items;
+       it += waves) {
+    const int64_t t = it / a.parts;
+    const int part = (int)(it - t * a.parts);
+    const int pos = (int)uniform32((uint32_t)a.positions[t]);
+    const int slot = (int)uniform32((uint32_t)a.slots[t]);
+    const bool live = a.rot ? pos >= 0 && pos < a.max_positions : pos >= 0;
+    const int64_t page = slot < 0 ? -1 : slot / a.page_size;
+    const bool stored = live && page >= 0 && page < a.pages;
+    const int64_t at = stored ? page * a.page_stride + (slot - page * a.page_size) * a.token_stride : 0;
+    if (live && r.turned) {
+      const float* cs = a.cos_sin + (int64_t)pos * a.rot;
+      if (a.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          r.cs[i] = cs[e0 / 2 + i];
+          r.sn[i] = cs[half + e0 / 2 + i];
+        }
+      } else {
+        const int p0 = r.upper ? e0 - half : e0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          r.cs[i] = cs[p0 + i];
+          r.sn[i] = cs[half + p0 + i];
+        }
+      }
+    }
+    const int s0 = steps * part / a.parts, s1 = steps * (part + 1) / a.parts;
+    for (int s = s0; s < s1; ++s) {
+      if (s < qs) {
+        const int h = s * kHeads + g;
+        const bool on = mine && h < a.heads;
+        u32x4_t w = {0, 0, 0, 0};
+        if (on && live)
+          w = *reinterpret_cast<const u32x4_t*>(a.q + t * a.q_stride + (int64_t)h * a.d + e0);
+        if (live)
+          w = norm_turn<T, LPH>(w, norm_q, qw, qp, r, a.d, a.eps, a.rot, a.interleaved);
+        if (on)
+          *reinterpret_cast<u32x4_t*>(a.q_out + (t * a.heads + h) * a.d + e0) = w;
+      } else {
+        if (!stored) break;
+        const bool is_k = s < qs + ks;
+        const int h = (is_k ? s - qs : s - qs - ks) * kHeads + g;
+        const bool on = mine && h < a.kv_heads;
+        u32x4_t w = {0, 0, 0, 0};
+        const uint16_t* src = is_k ? a.k + t * a.k_stride : a.v + t * a.v_stride;
+        if (on) w = *reinterpret_cast<const u32x4_t*>(src + (int64_t)h * a.d + e0);
+        if (is_k) w = norm_turn<T, LPH>(w, norm_k, kw, kp, r, a.d, a.eps, a.rot, a.interleaved);
+        uint16_t* dst = (is_k ? a.k_cache : a.v_cache) + at + (int64_t)h * a.head_stride;
+        if (on) *reinterpret_cast<u32x4_t*>(dst + e0) = w;
+      }
+    }
+  }
+}
+
+template <typename T>
+void launch_rope(const RopeArgs& a, hipStream_t stream) {
+  const int64_t items = a.tokens * a.parts, per = kRopeThreads / kWave;
+  const int64_t want = (items + per - 1) / per;
+  const dim3 grid((unsigned)(want < 4096 ? want : 4096));
+  if (a.d <= 64)
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 8>), grid, dim3(kRopeThreads), 0, stream, a);
+  else if (a.d <= 128)
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 16>), grid, dim3(kRopeThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 32>), grid, dim3(kRopeThreads), 0, stream, a);
+}
+
+}  // namespace
+}  // namespace lilicorr
+
+using namespace lilicorr;
+
+extern "C" lilicorr_status lilicorr_page_plan(
+    const int32_t* lengths, const int32_t* incoming, const int32_t* pages, int32_t* table,
+    int32_t* queue, const int64_t* cursor, int64_t N, int page_size, int64_t table_width,
+    int64_t queue_size, int64_t tokens, int64_t window, int64_t sinks, int32_t* pages_out,
+    int64_t* cursor_out, int32_t* starts, int32_t* totals, int32_t* slots, int32_t* positions,
+    hipStream_t stream) {
+  if (!lengths || !incoming || !pages || !table || !queue || !cursor || !pages_out || !cursor_out ||
+      !starts || !totals)
+    return LILICORR_ERR_INVALID_ARG;
+  if (N < 1 || page_size < 1 || table_width < 1 || queue_size < 1 || tokens < 0 || window < 0 ||
+      sinks < 0 || (sinks > 0 && window == 0))
+    return LILICORR_ERR_INVALID_ARG;
+  if (tokens > 0 && (!slots || !positions)) return LILICORR_ERR_INVALID_ARG;
+  if (pages_out == pages || cursor_out == cursor) return LILICORR_ERR_INVALID_ARG;
+  if (N > kPlanMaxN || page_size > 65536 || table_width > 0x7fffffffll / page_size ||
+      queue_size > 0x7fffffffll || tokens > 0x7fffffffll || window > 0x7fffffffll ||
+      sinks > 0x7fffffffll)
+    return LILICORR_ERR_UNSUPPORTED;
+  if (!aligned4(lengths) || !aligned4(incoming) || !aligned4(pages) || !aligned4(table) ||
+      !aligned4(queue) || !aligned8(cursor) || !aligned4(pages_out) || !aligned8(cursor_out) ||
+      !aligned4(starts) || !aligned4(totals) || !aligned4(slots) || !aligned4(positions))
+    return LILICORR_ERR_ALIGNMENT;
+  PlanArgs a;
+  a.lengths = lengths; a.incoming = incoming; a.pages = pages;
+  a.table = table; a.queue = queue; a.cursor = cursor;
+  a.N = (int)N; a.P = page_size; a.M = (int)table_width; a.C = (int)queue_size;
+  a.tokens = tokens; a.window = window;
+  a.first = (int)((sinks + page_size - 1) / page_size);
+  a.pages_out = pages_out; a.cursor_out = cursor_out;
+  a.starts = starts; a.totals = totals; a.slots = slots; a.positions = positions;
+  // a workgroup for 256 tokens; a batch without new tokens still has pages to give back
+  int64_t grid = (tokens + kPlanThreads - 1) / kPlanThreads;
+  if (grid < (N + 63) / 64) grid = (N + 63) / 64;
+  if (grid > 1024) grid = 1024;
+  hipLaunchKernelGGL(page_plan_kernel, dim3((unsigned)grid), dim3(kPlanThreads),
+                     3 * ((size_t)N + 1) * sizeof(int), stream, a);
+  return launch_status();
+}
+
+extern "C" lilicorr_status lilicorr_qk_norm_rope(
+    const void* q, int64_t q_stride, int heads, const void* k, int64_t k_stride, const void* v,
+    int64_t v_stride, int64_t tokens, const int32_t* slots, const int32_t* positions,
+    const float* cos_sin, int64_t max_positions, int rot, int interleaved, const float* q_weight,
+    const float* k_weight, float eps, const lilicorr_cache* cache, void* q_out,
+    hipStream_t stream) {
+  if (!cache) return LILICORR_ERR_INVALID_ARG;
+  if (const lilicorr_status s = cache_sizes(*cache)) return s;
+  if (heads < 1 || tokens < 0 || rot < 0 || rot > cache->d || max_positions < 0)
+    return LILICORR_ERR_INVALID_ARG;
+  if (rot > 0 && !cos_sin) return LILICORR_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || !isfinite(eps)) return LILICORR_ERR_INVALID_ARG;
+  if (q_stride < 0 || k_stride < 0 || v_stride < 0) return LILICORR_ERR_INVALID_ARG;
+  if (rot % 16 || heads > 65535 || tokens > 0x7fffffffll) return LILICORR_ERR_UNSUPPORTED;
+  if (tokens == 0) return LILICORR_OK;
+  if (!q || !k || !v || !slots || !positions || !q_out || !cache->k || !cache->v)
+    return LILICORR_ERR_INVALID_ARG;
+  // q rows that are turned in place must be laid out as the output is
+  if (q_out == q && q_stride != (int64_t)heads * cache->d) return LILICORR_ERR_INVALID_ARG;
+  if (!stride_ok(q_stride) || !stride_ok(k_stride) || !stride_ok(v_stride))
+    return LILICORR_ERR_ALIGNMENT;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) ||
+      !aligned16(cache->k) || !aligned16(cache->v) || (cos_sin && !aligned16(cos_sin)) ||
+      (q_weight && !aligned16(q_weight)) || (k_weight && !aligned16(k_weight)) ||
+      !aligned4(slots) || !aligned4(positions))
+    return LILICORR_ERR_ALIGNMENT;
+  RopeArgs a;
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
+  a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.tokens = tokens;
+  a.heads = heads; a.kv_heads = cache->heads; a.d = cache->d; a.rot = rot;
+  a.interleaved = interleaved != 0;
+  a.slots = slots; a.positions = positions; a.cos_sin = cos_sin; a.max_positions = max_positions;
+  a.q_weight = q_weight; a.k_weight = k_weight; a.eps = eps;
+  a.k_cache = (uint16_t*)cache->k; a.v_cache = (uint16_t*)cache->v; a.q_out = (uint16_t*)q_out;
+  a.pages = cache->pages; a.page_stride = cache->page_stride;
+  a.token_stride = cache->token_stride; a.head_stride = cache->head_stride;
+  a.page_size = cache->page_size;
+  // few tokens: their heads spread over more waves
+  a.parts = tokens >= 4096 ? 1 : tokens >= 512 ? 4 : 12;
+  if (cache->dtype == LILICORR_BF16) launch_rope<Bf16>(a, stream);
+  else launch_rope<F16>(a, stream);
+  return launch_status();
+}
