@@ -17,6 +17,7 @@ constexpr int kTargetItems = 512;  // workgroups that fill the chip: two on each
 // One pass over keys: which tile height, how many tiles and chunks
 struct Pass {
   int BM, tiles, chunk, chunks;
+  bool spread;
 };
 
 struct Plan {
@@ -50,6 +51,18 @@ Pass make_pass(int64_t rows_each, int64_t tiles, int heads, int64_t keys, int BM
   return p;
 }
 
+// the largest unit that page and token strides are whole multiples of: the kernels count offsets in it
+// in 32 bits, and a head's width or more is usual
+int64_t stride_unit(const lilicorr_cache& c) {
+  int64_t x = c.page_stride, y = c.token_stride;
+  while (y) {
+    const int64_t r = x % y;
+    x = y;
+    y = r;
+  }
+  return x ? x < (1 << 30) ? x : 8 : 8;
+}
+
 lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p) {
   if (const lilicorr_status s = cache_sizes(a.cache)) return s;
   if (a.tokens < 0 || a.N < 1 || a.table_width < 1 || a.heads < 1 || a.window < 0 || a.sinks < 0 ||
@@ -65,6 +78,10 @@ lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p
       a.table_width > kMost / a.cache.page_size || a.shared_length > kMost)
     return LILICORR_ERR_UNSUPPORTED;
   if (!stride_ok(a.q_stride)) return LILICORR_ERR_ALIGNMENT;
+  if ((double)a.cache.page_stride * (double)(a.cache.pages - 1) +
+          (double)a.cache.token_stride * (a.cache.page_size - 1) >=
+      4294967296.0 * (double)stride_unit(a.cache))
+    return LILICORR_ERR_UNSUPPORTED;
 
   const int64_t group = a.heads / a.cache.heads;
   const int64_t max_tokens = a.max_tokens < a.tokens ? a.max_tokens : a.tokens;
@@ -84,11 +101,13 @@ lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p
     if (seen < keys) keys = seen;
   }
   p.tail = make_pass(own, tiles, a.cache.heads, keys, BM);
+  p.tail.spread = own <= BM;
   p.slots = p.tail.chunks;
   if (shared) {
     const int64_t all = a.tokens * group;
     const int BS = tile_rows(all);
     p.first = make_pass(all, (all + BS - 1) / BS, a.cache.heads, a.shared_length, BS);
+    p.first.spread = false;
     p.slots += p.first.chunks;
   }
   const int64_t most_items = 0x7fffffffll / a.cache.heads;
@@ -110,23 +129,46 @@ void launch(const AttnArgs& a, int chunks, hipStream_t stream) {
                      dim3(C::kThreads), C::kLds, stream, a);
 }
 
+template <typename T, bool FULL, int DP>
+void launch_rows(const AttnArgs& a, const Pass& p, hipStream_t stream) {
+  if constexpr (DP == 64) {
+    if (p.BM == 32) launch<AttnConfig<T, FULL, 64, 1, 4, 1, 4>>(a, p.chunks, stream);
+    else if (p.BM == 64) launch<AttnConfig<T, FULL, 64, 2, 2, 1, 4>>(a, p.chunks, stream);
+    else launch<AttnConfig<T, FULL, 64, 4, 1, 2, 2>>(a, p.chunks, stream);
+  } else if constexpr (DP == 128) {
+    if (p.BM == 32) launch<AttnConfig<T, FULL, 128, 1, 4, 1, 2>>(a, p.chunks, stream);
+    else if (p.BM == 64) launch<AttnConfig<T, FULL, 128, 2, 2, 1, 2>>(a, p.chunks, stream);
+    else launch<AttnConfig<T, FULL, 128, 4, 1, 2, 2>>(a, p.chunks, stream);
+  } else {
+    if (p.BM == 32) launch<AttnConfig<T, FULL, 256, 1, 2, 1, 2>>(a, p.chunks, stream);
+    else if (p.BM == 64) launch<AttnConfig<T, FULL, 256, 2, 2, 1, 2>>(a, p.chunks, stream);
+    else launch<AttnConfig<T, FULL, 256, 4, 1, 1, 2>>(a, p.chunks, stream);
+  }
+}
+
 template <typename T>
 void launch_pass(AttnArgs a, const Pass& p, hipStream_t stream) {
   a.tiles = p.tiles;
   a.chunk = p.chunk;
+  a.spread = p.spread;
   if (a.d <= 64) {
-    if (p.BM == 32) launch<AttnConfig<T, 64, 1, 4, 1>>(a, p.chunks, stream);
-    else if (p.BM == 64) launch<AttnConfig<T, 64, 2, 2, 1>>(a, p.chunks, stream);
-    else launch<AttnConfig<T, 64, 4, 1, 2>>(a, p.chunks, stream);
+    if (a.d == 64) launch_rows<T, true, 64>(a, p, stream);
+    else launch_rows<T, false, 64>(a, p, stream);
   } else if (a.d <= 128) {
-    if (p.BM == 32) launch<AttnConfig<T, 128, 1, 4, 1>>(a, p.chunks, stream);
-    else if (p.BM == 64) launch<AttnConfig<T, 128, 2, 2, 1>>(a, p.chunks, stream);
-    else launch<AttnConfig<T, 128, 4, 1, 2>>(a, p.chunks, stream);
+    if (a.d == 128) launch_rows<T, true, 128>(a, p, stream);
+    else launch_rows<T, false, 128>(a, p, stream);
   } else {
-    if (p.BM == 32) launch<AttnConfig<T, 256, 1, 2, 1>>(a, p.chunks, stream);
-    else if (p.BM == 64) launch<AttnConfig<T, 256, 2, 2, 1>>(a, p.chunks, stream);
-    else launch<AttnConfig<T, 256, 4, 1, 1>>(a, p.chunks, stream);
+    if (a.d == 256) launch_rows<T, true, 256>(a, p, stream);
+    else launch_rows<T, false, 256>(a, p, stream);
   }
+}
+
+template <typename T, int LPR>
+void launch_join(const AttnArgs& a, const Plan& p, hipStream_t stream) {
+  constexpr int64_t per = kJoinThreads / kWave;
+  hipLaunchKernelGGL((attention_join_kernel<T, LPR>), dim3((unsigned)((p.rows + per - 1) / per)),
+                     dim3(kJoinThreads), 0, stream, a.part_o, a.part_ml, p.rows, p.slots, a.d,
+                     a.starts, a.N, a.tokens, a.heads, a.out);
 }
 
 template <typename T>
@@ -147,6 +189,10 @@ lilicorr_status run(const lilicorr_attention_args& x, const Plan& p, hipStream_t
   a.page_mul = (uint32_t)((((uint64_t)1 << a.page_shift) / c.page_size) + 1);
   a.tokens = (int)x.tokens; a.heads = x.heads; a.kv_heads = c.heads; a.group = x.heads / c.heads;
   a.d = c.d;
+  const int64_t unit = stride_unit(c);
+  a.page_units = (uint32_t)(c.page_stride / unit);
+  a.token_units = (uint32_t)(c.token_stride / unit);
+  a.unit_bytes = (uint32_t)(unit * 2);
   a.window = (int)(x.window < (1 << 30) ? x.window : (1 << 30));
   a.sinks = (int)(x.sinks < (1 << 30) ? x.sinks : (1 << 30));
   a.causal = x.causal != 0;
@@ -172,12 +218,9 @@ lilicorr_status run(const lilicorr_attention_args& x, const Plan& p, hipStream_t
   }
   launch_pass<T>(a, p.tail, stream);
   if (a.split) {
-    int lanes = 4;
-    while (lanes * 4 < c.d) lanes *= 2;
-    const int64_t per = kJoinThreads / lanes;
-    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((p.rows + per - 1) / per)),
-                       dim3(kJoinThreads), 0, stream, a.part_o, a.part_ml, p.rows, p.slots, c.d,
-                       lanes, a.starts, a.N, a.heads, a.out);
+    if (c.d <= 64) launch_join<T, 16>(a, p, stream);
+    else if (c.d <= 128) launch_join<T, 32>(a, p, stream);
+    else launch_join<T, 64>(a, p, stream);
   }
   return launch_status();
 }

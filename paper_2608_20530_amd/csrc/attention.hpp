@@ -15,14 +15,14 @@
 //
 // The keys that a tile sees are the first few (sinks) and a run (the window): one list, in which
 // position i is key i below the number of sinks and key i + shift above. Stages of 32 KB WK keys
-// of that list go to LDS by DMA, 16 bytes a lane from wherever the page table says, one stage
-// ahead of the products (page numbers one more), with one barrier a stage. Sixteen-byte pieces are
-// permuted within each row as they are copied so that the reads meet no bank conflicts.
+// of that list go to LDS by DMA, 16 bytes a lane from wherever the page table says, into a ring of
+// NS stages. Sixteen-byte pieces are permuted within each row as they are copied so that the reads
+// meet no bank conflicts. Where WR is 1 each wave copies just what it uses and meets no barrier.
 //
 // Softmax: running maximum and sum in fp32. The accumulated output is rescaled only when a
 // row's maximum has grown by more than 2^8 over the one that its powers are taken against (they
 // are then at most 2^8; fp32 sums and either 16-bit type hold that). Probabilities are rounded to
-// the cache's type for the matrix cores, the sum is of the unrounded ones.
+// the cache's type for the matrix cores, and the sum (fp32) is of the rounded ones, as the output is.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -44,7 +44,9 @@ typedef __attribute__((address_space(3))) u32x2_t* lds_u32x2_t;
 typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4_t;
 typedef __attribute__((address_space(3))) float* lds_float_t;
 typedef __attribute__((address_space(3))) int* lds_int_t;
+typedef __attribute__((address_space(3))) unsigned char* lds_t;
 
+constexpr int kWaitLoads = 0x0f70;  // s_waitcnt vmcnt(0) alone
 constexpr float kRescale = 8.f;  // growth of the maximum, in powers of two, that is let pass
 
 template <typename T>
@@ -64,14 +66,49 @@ __device__ __forceinline__ f32x16_t mfma<F16>(const u32x4_t& a, const u32x4_t& b
                                                 __builtin_bit_cast(x8, b), c, 0, 0, 0);
 }
 
+// c + a + b for the packed pair, in fp32
+template <typename T>
+__device__ __forceinline__ float add_pair(uint32_t w, float c);
+template <>
+__device__ __forceinline__ float add_pair<Bf16>(uint32_t w, float c) {
+  typedef __bf16 pair __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, 0x3f803f80u), c,
+                                         false);
+}
+template <>
+__device__ __forceinline__ float add_pair<F16>(uint32_t w, float c) {
+  typedef _Float16 pair __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, 0x3c003c00u), c, false);
+}
+
+// the largest of three; a NaN counts only beside NaNs
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  __asm__("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// bits at and above n, and below it, of 64 (any n)
+__device__ __forceinline__ uint64_t bits_from(int n) { return n <= 0 ? ~0ull : n >= 64 ? 0 : ~0ull << n; }
+__device__ __forceinline__ uint64_t bits_below(int n) { return ~bits_from(n); }
+
 // both halves of the wave see the larger of their value and the other half's
 __device__ __forceinline__ float cross_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return max3(__uint_as_float(r[0]), __uint_as_float(r[1]), -__builtin_inff());
 }
 __device__ __forceinline__ float cross_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// 16 bytes a lane from where each lane says to 1 KB of LDS in lane order, counted by vmcnt alone. Written
+// out because the compiler takes this instruction for one that LDS reads must wait for too: it made
+// every read of the loops wait for all that were under way (prefill 608 us with the builtin). No register
+// is loaded, so none is in flight.
+__device__ __forceinline__ void copy_to_lds(lds_t dst, const unsigned char* src) {
+  const uint32_t at = uniform32((uint32_t)(uintptr_t)dst);
+  __asm__ volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(at), "v"(src) : "memory");
 }
 
 struct AttnArgs {
@@ -84,18 +121,21 @@ struct AttnArgs {
   int N, table_width, pages, page_size;
   uint32_t page_mul, page_shift;  // n / page_size = (n * page_mul) >> page_shift
   int tokens, heads, kv_heads, group, d;
+  uint32_t page_units, token_units, unit_bytes;  // page and token strides in a common unit
   int window, sinks, causal;
   int max_tokens, max_length;
   int shared;            // 0, or the length of the shared keys, which this pass is for
   int tiles, chunk, slot0;  // keys of a chunk; slot of chunk 0
+  int spread;                       // XCDs take runs of items instead of every eighth
   int split;                        // whether partial results are written
   float scale2;                     // scale * log2 e
 };
 
-template <typename T_, int DP_, int WR_, int WK_, int KB_>
+template <typename T_, bool FULL_, int DP_, int WR_, int WK_, int KB_, int NS_>
 struct AttnConfig {
+  static constexpr bool FULL = FULL_;              // heads of DP elements, not fewer
   typedef T_ T;
-  static constexpr int DP = DP_, WR = WR_, WK = WK_, KB = KB_;
+  static constexpr int DP = DP_, WR = WR_, WK = WK_, KB = KB_, NS = NS_;
   static constexpr int kWaves = WR * WK, kThreads = kWaves * kWave;
   static constexpr int BM = 32 * WR;               // rows of a tile
   static constexpr int SK = 32 * KB * WK;          // keys of a stage
@@ -106,25 +146,33 @@ struct AttnConfig {
   static constexpr int IPW = WROWS / RPI;          // copy instructions for them, keys or values
   static constexpr int ND = DP / 32;               // output tiles
   static constexpr int LOOK = SK < kWave ? SK : kWave;  // keys whose page a wave looks up
-  static constexpr uint32_t kTile = SK * RB, kStage = 2 * kTile;
+  static constexpr bool kOwn = WR == 1;            // a wave copies just the keys that it uses
+  static constexpr uint32_t kTile = SK * RB, kStage = 2 * kTile, kRing = NS * kStage;
   static constexpr uint32_t kMerge = kWaves * 32 * DP * 4 + kWaves * kWave * 8;
-  static constexpr uint32_t kFlag = WK > 1 && kMerge > 2 * kStage ? kMerge : 2 * kStage;
-  static constexpr size_t kLds = kFlag + 16;       // and the word that calls for another try
+  // the ring, which the join of the waves uses again; each wave's part of the page table; the word
+  // that calls for another try
+  static constexpr uint32_t kPages = WK > 1 && kMerge > kRing ? kMerge : kRing;
+  static constexpr int kEntries = 256;
+  static constexpr uint32_t kFlag = kPages + kWaves * kEntries * 4;
+  static constexpr size_t kLds = kFlag + 16;
+  static_assert(KB <= 2, "blocks of a stage and wave");
   static_assert(WROWS % RPI == 0 && WROWS <= kWave, "whole copy instructions");
   static_assert(SK <= kWave || WR == 1, "a wave looks up the pages of what it copies and uses");
 };
 
-// which 16-byte piece of a row lies where: the keys' reads take one piece of 32 rows, the values'
-// transposing reads four pieces of four rows
+// Piece c of row r of a stage lies at place c ^ swizzle(r) of the row. The keys' reads take one piece of 32
+// rows, eight lanes a cycle: eight consecutive rows differ modulo 8, sixteen modulo 16. The values'
+// transposing reads take two neighbouring pieces of four consecutive rows with 16 lanes: those rows
+// differ in bits 1-2 (and the four pieces that 32 lanes take, in bits 2-3).
 template <int CPR>
-__device__ __forceinline__ uint32_t swizzle_k(uint32_t row) {
-  return row & (CPR < 16 ? CPR - 1 : 15);
+__device__ __forceinline__ uint32_t swizzle(uint32_t row) {
+  const uint32_t r = row & 3, k = row >> 2;
+  if (CPR < 16) return (r << 1) ^ (k & 1);
+  return (r << 2) ^ (((r ^ (r >> 1)) & 1) << 1) ^ (k & 1) ^ ((k & 2) << 2);
 }
-template <int CPR>
-__device__ __forceinline__ uint32_t swizzle_v(uint32_t row) {
-  const uint32_t r = row & 3;
-  return CPR >= 16 ? (r << 2) | ((r ^ (r >> 1)) & 1) << 1 : r << 1;
-}
+
+// what is copied past the width of heads that are narrower than DP
+__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
 
 // A chunk of the list of keys that a tile sees
 struct Keys {
@@ -188,8 +236,13 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   const int col = lane & 31, half = lane >> 5;
 
   // ---- which rows ------------------------------------------------------------------------------
-  const int head = item % a.kv_heads;
-  const int rest = item / a.kv_heads;
+  int it = item;
+  if (a.spread) {
+    const int per = (int)gridDim.x / 8;
+    if (it < per * 8) it = (it % 8) * per + it / 8;
+  }
+  const int head = it % a.kv_heads;
+  const int rest = it / a.kv_heads;
   const int chunk_no = rest / a.tiles;
   // long rows first: with a causal mask and no window the last tiles of a request see most
   const int tile = a.tiles - 1 - rest % a.tiles;
@@ -246,7 +299,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   const int tok = rowc / a.group;
   const int64_t orow = ((int64_t)start + tok) * a.heads + head * a.group + (rowc - tok * a.group);
   const int p = pos0 + tok;  // its position: it sees the keys from j_least to j_most, and the sinks
-  const int j_most = a.causal ? p : 0x7fffffff, j_least = a.window ? p - a.window + 1 : -0x7fffffff;
+  const int j_most = a.causal ? p : 0x3fffffff, j_least = a.window ? p - a.window + 1 : -0x3fffffff;
   if (v_begin >= nv && chunk_no > 0) {  // (chunk 0 of a tile without keys writes its zeros below)
     if (wk == 0 && half == 0 && row < r1)
       a.part_ml[(int64_t)(a.slot0 + chunk_no) * a.rows + orow] = f32x2_t{-__builtin_inff(), 0.f};
@@ -254,7 +307,6 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   }
   // the wave's rows, for the whole block's sake: positions of its first and last
   const int wrow0 = r0 + wr * 32;
-  const bool has_rows = wrow0 < r1;
   const int wp_lo = pos0 + min(wrow0, r1 - 1) / a.group;
   const int wp_hi = pos0 + min(wrow0 + 31, r1 - 1) / a.group;
 
@@ -273,42 +325,67 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   // ---- copies ------------------------------------------------------------------------------------
   const uint16_t* kbase = a.k + (int64_t)head * a.head_stride;
   const uint16_t* vbase = a.v + (int64_t)head * a.head_stride;
+  const unsigned char *kbytes = (const unsigned char*)kbase, *vbytes = (const unsigned char*)vbase;
   const int32_t* trow = a.table + (int64_t)n * a.table_width;
-  constexpr int kLookBase = C::SK <= kWave ? 0 : 1;  // stages wider than a wave: each its own part
-  const int look0 = kLookBase ? wave * C::WROWS : 0;
-  // pages of the list's positions v0 + look0 + lane; positions past the end take the last key
-  struct Look { int page, off; };
-  auto look = [&](int v0) {
-    const int i = min(v0 + look0 + (lane < C::LOOK ? lane : 0), v_end - 1);
-    const int j = i < ns ? i : i + shift;
-    const int e = (int)(((uint64_t)(uint32_t)j * a.page_mul) >> a.page_shift);
-    return Look{trow[e], j - e * a.page_size};
+  // The page numbers of the list's positions, in LDS: the entries of the sinks, then those of the
+  // window. A wave keeps kEntries of them, from number x0 on, and fetches the next ones when a stage
+  // runs out of them, so that page numbers are not waited for among the copies.
+  const int look0 = C::SK <= kWave ? 0 : wave * C::WROWS;
+  const int xs = (ns + a.page_size - 1) / a.page_size;
+  auto entry_of = [&](int j) { return (int)(((uint64_t)(uint32_t)j * a.page_mul) >> a.page_shift); };
+  const int e_lo = entry_of(lo);
+  auto number_of = [&](int i, int e) { return i < ns ? e : e - e_lo + xs; };
+  const uint32_t tab = C::kPages + wave * (C::kEntries * 4);
+  int x0 = 0;
+  bool absent = false;  // a page among those so far is not there
+  auto fetch = [&](int x, int x_last) {
+    x0 = x;
+#pragma unroll
+    for (int u = 0; u < C::kEntries / kWave; ++u) {
+      const int y = min(x + u * kWave + lane, x_last);
+      const int page = trow[y < xs ? y : y - xs + e_lo];
+      absent |= __ballot(page < 0 || page >= a.pages) != 0;
+      *(lds_int_t)(smem + tab + (u * kWave + lane) * 4) = page;
+    }
   };
-  auto present = [&](const Look& w) { return w.page >= 0 && w.page < a.pages; };
+  const int x_last = v_end > 0 ? number_of(v_end - 1, entry_of(v_end - 1 < ns ? v_end - 1 : v_end - 1 + shift)) : 0;
   const int my_row = lane / C::CPR, my_pos = lane % C::CPR;
-  auto copy = [&](const Look& w, int s) {
-    const int64_t at = present(w) ? (int64_t)w.page * a.page_stride + (int64_t)w.off * a.token_stride : 0;
-    unsigned char* dst = smem + (uint32_t)(s & 1) * C::kStage + (uint32_t)(wave * C::WROWS) * C::RB;
+  // Where the rows of the stage whose first position is v0 lie, for the copies of this wave; positions
+  // past the end take the last key. It is asked for a stage ahead of the copies, among the products.
+  typedef uint32_t places_t __attribute__((ext_vector_type(C::IPW)));
+  auto prepare = [&](int v0) __attribute__((always_inline)) {
+    auto key_at = [&](int i) { return i < ns ? i : i + shift; };
+    const int first = min(v0 + look0, v_end - 1), last = min(v0 + look0 + C::LOOK - 1, v_end - 1);
+    if (number_of(last, entry_of(key_at(last))) >= x0 + C::kEntries)
+      fetch(number_of(first, entry_of(key_at(first))), x_last);
+    const int i = min(v0 + look0 + (C::LOOK < kWave && lane >= C::LOOK ? 0 : lane), v_end - 1);
+    const int j = key_at(i), e = entry_of(j);
+    int page = *(lds_int_t)(smem + tab + (number_of(i, e) - x0) * 4);
+    if (absent && (page < 0 || page >= a.pages)) page = 0;
+    const uint32_t at = (uint32_t)page * a.page_units + (uint32_t)(j - e * a.page_size) * a.token_units;
+    places_t to;
+#pragma unroll
+    for (int i = 0; i < C::IPW; ++i)
+      to[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(
+          (wave * C::WROWS + i * C::RPI + my_row - look0) * 4, (int)at);
+    return to;
+  };
+  // and their copies, to the place at `ring`
+  auto copy = [&](const places_t from, lds_t ring) __attribute__((always_inline)) {
+    const lds_t dst = ring + (uint32_t)(wave * C::WROWS) * C::RB;
 #pragma unroll
     for (int i = 0; i < C::IPW; ++i) {
       const int r = wave * C::WROWS + i * C::RPI + my_row;  // row of the stage
-      const int64_t src = (int64_t)shfl64((uint64_t)at, r - look0);
-      const uint32_t ck = my_pos ^ swizzle_k<C::CPR>(r), cv = my_pos ^ swizzle_v<C::CPR>(r);
-      // past the head's width nothing is copied: the zeros put there before stay
-      if ((int)ck * 8 < a.d)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kbase + src + ck * 8),
-                                         (lds_void_t)(dst + i * 1024), 16, 0, 0);
-      if ((int)cv * 8 < a.d)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vbase + src + cv * 8),
-                                         (lds_void_t)(dst + C::kTile + i * 1024), 16, 0, 0);
+      const uint32_t piece = my_pos ^ swizzle<C::CPR>(r);
+      const unsigned char* ks = kbytes + piece * 16 + (uint64_t)from[i] * a.unit_bytes;
+      const unsigned char* vs = ks + (vbytes - kbytes);
+      if constexpr (!C::FULL) {
+        if ((int)piece * 8 >= a.d) ks = vs = (const unsigned char*)kZeros;
+      }
+      copy_to_lds(dst + i * 1024, ks);
+      copy_to_lds(dst + C::kTile + i * 1024, vs);
     }
   };
-
-  if (a.d < C::DP) {
-    for (uint32_t i = tid * 16; i < 2 * C::kStage; i += C::kThreads * 16)
-      *(lds_u32x4_t)(smem + i) = u32x4_t{0, 0, 0, 0};
-    __syncthreads();
-  }
 
   const auto again = (lds_int_t)(smem + C::kFlag);
   if (tid == 0) *again = 0;  // before the first stage's barrier; read after the last one's
@@ -322,125 +399,215 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   // LDS offsets of this lane's reads, without the stage
   const uint32_t sub = (uint32_t)wk * (C::KB * 32);  // first key of the wave's share of a stage
   const uint32_t k_at = (sub + col) * C::RB;
-  const uint32_t k_x = half ^ swizzle_k<C::CPR>(col);
+  const uint32_t k_x = half ^ swizzle<C::CPR>(col);
   const uint32_t v_row = 4 * half + ((lane & 15) >> 2);
   const uint32_t v_at = C::kTile + (sub + v_row) * C::RB + (lane & 1) * 8;
   const uint32_t v_c = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-  const uint32_t v_x = swizzle_v<C::CPR>(v_row);
+  const uint32_t v_x = swizzle<C::CPR>(v_row);
 
   const int stages = v_end > v_begin ? (v_end - v_begin + C::SK - 1) / C::SK : 0;
-  Look next = {0, 0}, cur = {0, 0};
+  // The first page numbers, and with them everything asked for so far: the products below find their
+  // operands there and wait for nothing but the copies.
   if (stages) {
-    cur = look(v_begin);
-    copy(cur, 0);
-    next = look(v_begin + C::SK);
+    const int first = min(v_begin + look0, v_end - 1);
+    fetch(number_of(first, entry_of(first < ns ? first : first + shift)), x_last);
   }
-  for (int s = 0; s < stages; ++s) {
-    const uint64_t have = __ballot(present(cur) || lane >= C::LOOK);
-    // this wave's copies have landed, then everyone's; and all waves are done with the other buffer
-    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (s + 1 < stages) {
-      copy(next, s + 1);
-      cur = next;
-      next = look(v_begin + (s + 2) * C::SK);
+  __builtin_amdgcn_s_waitcnt(kWaitLoads);
+  if constexpr (C::kOwn) __syncthreads();  // `again` is 0 before any wave sets it
+#pragma unroll
+  for (int s = 0; s < C::NS - 1; ++s)
+    if (s < stages) {
+      copy(prepare(v_begin + s * C::SK), (lds_t)smem + s * C::kStage);
     }
+  places_t from = {};
+  if (C::NS - 1 < stages) from = prepare(v_begin + (C::NS - 1) * C::SK);
+  constexpr int kAhead = C::kOwn ? C::NS - 1 : C::NS - 2;  // stages under way while this one is waited for
+  // stage s, which lies at st, while a later one is copied to nx
+  auto stage = [&](const lds_t st, const lds_t nx, int s) __attribute__((always_inline)) {
+    const bool more = s + C::NS - 1 < stages;
+    // a wave that uses its own copies alone begins the next one and waits for its oldest; otherwise
+    // the barrier says that everyone's copies have landed and that all are done with the place that the
+    // next ones overwrite
+    __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last stage's reads
+    if constexpr (C::kOwn) {
+      if (more) copy(from, nx);
+    }
+    if (C::kOwn ? more : s + C::NS - 2 < stages)
+      __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead * 2 * C::IPW) : "memory");
+    else
+      __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (!C::kOwn) {
+      __asm__ volatile("s_barrier" ::: "memory");
+      if (more) copy(from, nx);
+    }
+    const bool later = s + C::NS < stages;
     const int v0 = v_begin + s * C::SK + (int)sub;
-    if (!has_rows || v0 >= v_end) continue;
     constexpr int kKeys = C::KB * 32;
     const int j_lo = v0 < ns ? v0 : v0 + shift, j_hi = v0 + kKeys - 1 + shift;
-    if (v0 >= ns && ((a.causal && j_lo > wp_hi) || (a.window && j_hi <= wp_lo - a.window && j_lo >= a.sinks)))
-      continue;  // no row of the wave sees any of it
     constexpr uint64_t kAll = kKeys == 64 ? ~0ull : ((1ull << kKeys) - 1);
-    uint64_t here = (have >> (C::SK <= kWave ? (int)sub : 0)) & kAll;  // list positions with a key
-    if (v_end - v0 < kKeys) here &= (1ull << (v_end - v0)) - 1;
+    uint64_t here = kAll;  // list positions with a key
+    if (absent) {
+      const int i = min(v0 + (lane < kKeys ? lane : 0), v_end - 1);
+      const int page = trow[entry_of(i < ns ? i : i + shift)];
+      here &= __ballot(page >= 0 && page < a.pages);
+    }
+    here &= bits_below(v_end - v0);
     const bool whole = here == kAll && (v0 >= ns || shift == 0) &&
                        (!a.causal || j_hi <= wp_lo) && (!a.window || j_lo > wp_hi - a.window);
-    unsigned char* st = smem + (uint32_t)(s & 1) * C::kStage;
-
-    // scores
-    f32x16_t sc[C::KB];
-#pragma unroll
-    for (int b = 0; b < C::KB; ++b) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < C::DP / 16; ++i) {
-        const u32x4_t kf = *(lds_u32x4_t)(st + k_at + b * 32 * C::RB + ((k_x ^ (2 * i)) * 16));
-        sc[b] = mfma<T>(kf, q[i], sc[b]);
-      }
-    }
-    auto key_of = [&](int b, int e) { return v0 + b * 32 + 8 * (e >> 2) + 4 * half + (e & 3); };
-    auto sees = [&](int v) {  // this lane's row and the list's position v
-      const int j = v < ns ? v : v + shift;
-      return ((here >> (v - v0)) & 1) && j <= j_most && (j >= j_least || j < a.sinks);
-    };
+    // the list's positions v0 .. that this lane's row sees: of the sinks' part keys up to its own, of
+    // the window's part its window, and sinks that lie in it
+    uint64_t vis = 0;
     if (!whole) {
+      const uint64_t part = bits_below(ns - v0);
+      const int w0 = v0 + shift;
+      vis = here & ((part & bits_below(j_most + 1 - v0)) |
+                    (~part & bits_below(j_most + 1 - w0) & (bits_from(j_least - w0) | bits_below(a.sinks - w0))));
+      vis >>= 4 * half;
+    }
+    // Blocks of 32 keys. While one block's powers are taken, the matrix cores have the next block's
+    // scores or the last one's output to do: the two are laid out in steps of one matrix instruction
+    // each, with operands read three steps ahead, and the scheduler is held to that.
+    constexpr int kQK = C::DP / 16, kPV = 2 * C::ND;  // steps of a block
+    f32x16_t sc[C::KB];
+    u32x4_t pf[C::KB * 2], kf[4], vf[4];
+    auto load_k = [&](int x) {  // operand x % kQK of block x / kQK
+      if (x < kQK * C::KB)
+        kf[x & 3] = *(lds_u32x4_t)(st + k_at + (x / kQK) * 32 * C::RB + ((k_x ^ (2 * (x % kQK))) * 16));
+    };
+    auto load_v = [&](int x) {  // operand of 16 keys x / ND and output tile x % ND
+      if (x >= kPV * C::KB) return;
 #pragma unroll
-      for (int b = 0; b < C::KB; ++b)
+      for (int y = 0; y < 2; ++y) {
+        // rows eight apart differ in bit 3 of the swizzle, rows sixteen apart not at all
+        const uint32_t place = (4 * (x % C::ND) + v_c) ^ v_x ^ (C::CPR < 16 ? 0 : 8 * y);
+        const uint32_t at = v_at + (16 * (x / C::ND) + 8 * y) * C::RB + place * 16;
+        const u32x2_t w = __builtin_bit_cast(
+            u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(st + at)));
+        vf[x & 3][2 * y] = w[0];
+        vf[x & 3][2 * y + 1] = w[1];
+      }
+    };
+    auto score_step = [&](int b, int i) {
+      load_k(b * kQK + i + 3);
+      if (i == 0) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
+      }
+      sc[b] = mfma<T>(kf[(b * kQK + i) & 3], q[i], sc[b]);
+    };
+    auto output_step = [&](int b, int i) {
+      load_v(b * kPV + i + 3);
+      o[i % C::ND] = mfma<T>(vf[(b * kPV + i) & 3], pf[2 * b + i / C::ND], o[i % C::ND]);
+    };
+    float ms = 0.f;
+    auto power_step = [&](int b, int e0, int n) {
+#pragma unroll
+      for (int e = e0; e < e0 + n; ++e) {
+        sc[b][e] = __builtin_amdgcn_exp2f(fmaf(sc[b][e], a.scale2, -ms));
+        if (e & 1) {
+          uint32_t w = T::pack(sc[b][e - 1], sc[b][e]);
+          l = add_pair<T>(w, l);
+          __asm__ volatile("" : "+v"(w), "+v"(l));  // here and not later
+          pf[b * 2 + (e >> 3)][(e & 7) >> 1] = w;
+        }
+      }
+    };
+    // masks the block's scores and brings the maximum up to it
+    auto maximum = [&](int b) {
+      if (!whole) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          sc[b][e] = sees(key_of(b, e)) ? sc[b][e] : -__builtin_inff();
+          sc[b][e] = (uint32_t)(vis >> (b * 32)) & (1u << (8 * (e >> 2) + (e & 3))) ? sc[b][e] : -__builtin_inff();
+      }
+      float mx = sc[b][0];
+#pragma unroll
+      for (int e = 1; e < 15; e += 2) mx = max3(mx, sc[b][e], sc[b][e + 1]);
+      mx = cross_max(max3(mx, sc[b][15], mx));
+      const bool grows = (mx - m) * a.scale2 > kRescale;  // -inf - -inf is NaN and does not count
+      if (__ballot(grows)) {
+        // nothing is accumulated while m is -inf; rows that need not change keep their values exactly
+        const float f = !grows ? 1.f : m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mx) * a.scale2);
+        m = grows ? mx : m;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < C::ND; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[i][e] *= f;
+        if (b > 0) {  // the block before has its powers but is not in the output yet
+#pragma unroll
+          for (int w = 0; w < 8; ++w) {
+            const f32x2_t v = T::unpack(pf[(b - 1) * 2 + (w >> 2)][w & 3]);
+            pf[(b - 1) * 2 + (w >> 2)][w & 3] = T::pack(v[0] * f, v[1] * f);
+          }
+        }
+      }
+    };
+    load_k(0);
+    load_k(1);
+    load_k(2);
+#pragma unroll
+    for (int i = 0; i < kQK; ++i) {
+      score_step(0, i);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    // maximum
-    float mx = sc[0][0];
-#pragma unroll
-    for (int b = 0; b < C::KB; ++b)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[b][e]);
-    mx = cross_max(mx);
-    if (__ballot((mx - m) * a.scale2 > kRescale)) {  // -inf - -inf is NaN and does not count
-      const float grown = fmaxf(m, mx);
-      // nothing is accumulated while m is -inf
-      const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - grown) * a.scale2);
-      m = grown;
-      l *= f;
-#pragma unroll
-      for (int i = 0; i < C::ND; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] *= f;
-    }
-    const float ms = m == -__builtin_inff() ? 0.f : m * a.scale2;
-    u32x4_t pf[C::KB * 2];
+    if (later) from = prepare(v_begin + (s + C::NS) * C::SK);
 #pragma unroll
     for (int b = 0; b < C::KB; ++b) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        sc[b][e] = __builtin_amdgcn_exp2f(fmaf(sc[b][e], a.scale2, -ms));
-        l += sc[b][e];
+      if (b == C::KB - 1) {
+        load_v(0);
+        load_v(1);
+        load_v(2);
       }
+      maximum(b);
+      ms = m == -__builtin_inff() ? 0.f : m * a.scale2;
+      if (b + 1 < C::KB) {
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) pf[b * 2 + (e >> 3)][(e & 7) >> 1] = T::pack(sc[b][e], sc[b][e + 1]);
+        for (int i = 0; i < kQK; ++i) {
+          score_step(b + 1, i);
+          power_step(b, i * (16 / kQK), 16 / kQK);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else if (b > 0) {
+#pragma unroll
+        for (int i = 0; i < kPV; ++i) {
+          output_step(b - 1, i);
+          power_step(b, i * (16 / kPV), 16 / kPV);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
+        power_step(b, 0, 16);
+      }
     }
     // A value that is not finite, in a key that some row does not see, must not reach that row, but
     // 0 * inf is NaN. Rare enough for the whole tile to be done again another way.
     if (!whole) {
       constexpr int kReads = kKeys / C::RPI;
       uint32_t any = 0;
-#pragma unroll 4
+#pragma unroll 1
       for (int i = 0; i < kReads; ++i) {
         const u32x4_t w = *(lds_u32x4_t)(st + C::kTile + sub * C::RB + i * 1024 + lane * 16);
         any |= T::nonfinite(w[0]) | T::nonfinite(w[1]) | T::nonfinite(w[2]) | T::nonfinite(w[3]);
       }
       if (any) *again = 1;
     }
-    // output
-    auto v_frag = [&](int g, int t) {
-      const uint32_t at = v_at + 16 * g * C::RB + (((4 * t + v_c) ^ v_x) * 16);
-      u32x4_t vf;
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const u32x2_t w = __builtin_bit_cast(
-            u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(st + at + 8 * y * C::RB)));
-        vf[2 * y] = w[0];
-        vf[2 * y + 1] = w[1];
-      }
-      return vf;
-    };
-#pragma unroll
-    for (int g = 0; g < C::KB * 2; ++g)
-#pragma unroll
-      for (int t = 0; t < C::ND; ++t) o[t] = mfma<T>(v_frag(g, t), pf[g], o[t]);
+    for (int i = 0; i < kPV; ++i) {
+      output_step(C::KB - 1, i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if constexpr (C::NS == 2 && C::kRing <= 65536) {  // places that fit the reads' immediate offsets
+    for (int s = 0; s < stages; s += 2) {
+      stage((lds_t)smem, (lds_t)smem + C::kStage, s);
+      if (s + 1 < stages) stage((lds_t)smem + C::kStage, (lds_t)smem, s + 1);
+    }
+  } else {
+    uint32_t ring = 0, ring_new = (C::NS - 1) * C::kStage;
+    for (int s = 0; s < stages; ++s) {
+      stage((lds_t)smem + ring, (lds_t)smem + ring_new, s);
+      ring = ring + C::kStage == C::kRing ? 0 : ring + C::kStage;
+      ring_new = ring_new + C::kStage == C::kRing ? 0 : ring_new + C::kStage;
+    }
   }
 
   __syncthreads();  // the last stage has been read, and `again` written
@@ -536,36 +703,65 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
 }
 
 template <typename C>
-__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::DP > 128 ? 1 : 2)))
+__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::DP > 128 ? 1 : 2, C::DP > 128 ? 1 : 2)))
 void attention_kernel(AttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char attn_smem[];
   attention_tile<C>(a, (int)blockIdx.x, attn_smem);
 }
 
-// Joins the slots of every row in their order: one row for d / 4 lanes.
+// Joins the slots of every row in their order, a wave a row: maxima and sums one lane a slot, then the
+// partial outputs in 16 bytes a lane, LPR lanes a slot and 64 / LPR slots at once.
 constexpr int kJoinThreads = 256;
-template <typename T>
+template <typename T, int LPR>
 __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(
     const float* __restrict__ part_o, const f32x2_t* __restrict__ part_ml, int64_t rows, int slots,
-    int d, int lanes, const int32_t* __restrict__ starts, int N, int heads, uint16_t* out) {
-  const int64_t per = kJoinThreads / lanes;
-  const int64_t row = blockIdx.x * per + threadIdx.x / lanes;
-  const int x = (threadIdx.x % lanes) * 4;
-  const int64_t used = (int64_t)starts[N] * heads;
-  if (row >= rows || row >= used || x >= d) return;
+    int d, const int32_t* __restrict__ starts, int N, int tokens, int heads,
+    uint16_t* __restrict__ out) {
+  constexpr int kAtOnce = kWave / LPR;
+  const int lane = lane_id();
+  const int64_t row = (int64_t)blockIdx.x * (kJoinThreads / kWave) + threadIdx.x / kWave;
+  const int x = (lane % LPR) * 4;
+  if (row >= rows || row >= (int64_t)min(max(starts[N], 0), tokens) * heads) return;
   float top = -__builtin_inff(), l = 0.f;
-  for (int s = 0; s < slots; ++s) top = fmaxf(top, part_ml[s * rows + row][0]);
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < slots; ++s) {
-    const f32x2_t ml = part_ml[s * rows + row];
-    if (ml[1] == 0.f) continue;  // saw nothing; a NaN stays one
-    const float f = ml[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
-    l += f * ml[1];
-    o += f * *reinterpret_cast<const f32x4_t*>(part_o + (s * rows + row) * d + x);
+  for (int s0 = 0; s0 < slots; s0 += kWave) {
+    f32x2_t ml = {-__builtin_inff(), 0.f};
+    if (s0 + lane < slots) ml = part_ml[(s0 + lane) * rows + row];
+    const float grown = fmaxf(top, wave_max_dpp(ml[0]));
+    const float f0 = top == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(top - grown);
+    // a slot that saw nothing has the sum 0; a NaN stays one
+    const float f = ml[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[0] - grown);
+    const bool saw = ml[1] != 0.f;
+    top = grown;
+    l = l * f0 + wave_sum_dpp(saw ? f * ml[1] : 0.f);
+    o *= f0;
+    const uint64_t which = __ballot(saw);
+    const int here = min(slots - s0, kWave);
+    constexpr int kBatch = 8;
+    for (int b = 0; b < here; b += kBatch * kAtOnce) {
+      f32x4_t v[kBatch];
+      float w[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int s = b + u * kAtOnce + lane / LPR;
+        const bool on = s < here && ((which >> (s & 63)) & 1) && x < d;
+        w[u] = __shfl(f, s & 63, kWave);
+        v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (on) v[u] = *reinterpret_cast<const f32x4_t*>(part_o + ((s0 + s) * rows + row) * d + x);
+        if (!on) w[u] = 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) o += w[u] * v[u];
+    }
   }
+#pragma unroll
+  for (int m = LPR; m < kWave; m <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m, kWave);
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  *reinterpret_cast<u32x2_t*>(out + row * d + x) =
-      u32x2_t{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
+  if (lane < LPR && x < d)
+    *reinterpret_cast<u32x2_t*>(out + row * d + x) =
+        u32x2_t{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
 }
 
 }  // namespace
