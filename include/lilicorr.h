@@ -478,7 +478,8 @@ lilicorr_status lilicorr_scorer_forward(float *X, int64_t N, int64_t S, int K, i
  * Lengths, tables and slots live on the device and are made there, so that a step needs no host
  * synchronisation. A wrong index there costs no memory safety: a page outside [0, pages) is a page
  * that is not there, and everything else is clamped. Index arrays need only their type's alignment
- * (LILICORR_ERR_ALIGNMENT otherwise), everything else 16 bytes.
+ * (LILICORR_ERR_ALIGNMENT otherwise), everything else 16 bytes. Each call takes a host struct of its
+ * arguments, read before the call returns.
  */
 
 /*
@@ -507,13 +508,17 @@ lilicorr_status lilicorr_scorer_forward(float *X, int64_t N, int64_t S, int K, i
  * Drafts that were rejected need nothing: call with the shorter length, the pages stay.
  * Limits: 1 <= N <= 4096, 1 <= P <= 65536, P * M < 2^31, 0 <= tokens < 2^31, C < 2^31.
  */
-lilicorr_status lilicorr_page_plan(const int32_t *lengths, const int32_t *incoming,
-                                   const int32_t *pages, int32_t *table, int32_t *queue,
-                                   const int64_t *cursor, int64_t N, int page_size,
-                                   int64_t table_width, int64_t queue_size, int64_t tokens,
-                                   int64_t window, int64_t sinks, int32_t *pages_out,
-                                   int64_t *cursor_out, int32_t *starts, int32_t *totals,
-                                   int32_t *slots, int32_t *positions, hipStream_t stream);
+typedef struct {
+    const int32_t *lengths, *incoming, *pages;
+    int32_t *table, *queue;
+    const int64_t *cursor;
+    int32_t *pages_out;
+    int64_t *cursor_out;
+    int32_t *starts, *totals, *slots, *positions;
+    int64_t N, page_size, table_width, queue_size, tokens, window, sinks;
+} lilicorr_page_plan_args;
+
+lilicorr_status lilicorr_page_plan(const lilicorr_page_plan_args *args, hipStream_t stream);
 
 /* The cache: element x of head h of the token at place o of page p lies at
  * p * page_stride + o * token_stride + h * head_stride + x of k (keys) and of v (values). Strides are
@@ -547,14 +552,18 @@ typedef struct {
  * Two tokens of a call must not have the same slot. Limits: rot a multiple of 16, 0 <= rot <= d
  * (cos_sin may be NULL when 0); tokens < 2^31.
  */
-lilicorr_status lilicorr_qk_norm_rope(const void *q, int64_t q_stride, int heads, const void *k,
-                                      int64_t k_stride, const void *v, int64_t v_stride,
-                                      int64_t tokens, const int32_t *slots,
-                                      const int32_t *positions, const float *cos_sin,
-                                      int64_t max_positions, int rot, int interleaved,
-                                      const float *q_weight, const float *k_weight, float eps,
-                                      const lilicorr_cache *cache, void *q_out,
-                                      hipStream_t stream);
+typedef struct {
+    const void *q, *k, *v;
+    void *q_out;
+    lilicorr_cache cache;
+    const int32_t *slots, *positions;
+    const float *cos_sin, *q_weight, *k_weight;
+    int64_t q_stride, k_stride, v_stride, tokens, max_positions;
+    int heads, rot, interleaved;
+    float eps;
+} lilicorr_qk_norm_rope_args;
+
+lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_args *args, hipStream_t stream);
 
 /*
  * Attention over the paged cache. Request n has T = starts[n+1] - starts[n] queries (rows starts[n] ..

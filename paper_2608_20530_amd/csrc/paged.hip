@@ -396,86 +396,84 @@ void launch_rope(const RopeArgs& a, hipStream_t stream) {
 
 using namespace lilicorr;
 
-extern "C" lilicorr_status lilicorr_page_plan(
-    const int32_t* lengths, const int32_t* incoming, const int32_t* pages, int32_t* table,
-    int32_t* queue, const int64_t* cursor, int64_t N, int page_size, int64_t table_width,
-    int64_t queue_size, int64_t tokens, int64_t window, int64_t sinks, int32_t* pages_out,
-    int64_t* cursor_out, int32_t* starts, int32_t* totals, int32_t* slots, int32_t* positions,
-    hipStream_t stream) {
-  if (!lengths || !incoming || !pages || !table || !queue || !cursor || !pages_out || !cursor_out ||
-      !starts || !totals)
+extern "C" lilicorr_status lilicorr_page_plan(const lilicorr_page_plan_args* args,
+                                              hipStream_t stream) {
+  if (!args) return LILICORR_ERR_INVALID_ARG;
+  const lilicorr_page_plan_args& x = *args;
+  if (!x.lengths || !x.incoming || !x.pages || !x.table || !x.queue || !x.cursor || !x.pages_out ||
+      !x.cursor_out || !x.starts || !x.totals)
     return LILICORR_ERR_INVALID_ARG;
-  if (N < 1 || page_size < 1 || table_width < 1 || queue_size < 1 || tokens < 0 || window < 0 ||
-      sinks < 0 || (sinks > 0 && window == 0))
+  if (x.N < 1 || x.page_size < 1 || x.table_width < 1 || x.queue_size < 1 || x.tokens < 0 ||
+      x.window < 0 || x.sinks < 0 || (x.sinks > 0 && x.window == 0))
     return LILICORR_ERR_INVALID_ARG;
-  if (tokens > 0 && (!slots || !positions)) return LILICORR_ERR_INVALID_ARG;
-  if (pages_out == pages || cursor_out == cursor) return LILICORR_ERR_INVALID_ARG;
-  if (N > kPlanMaxN || page_size > 65536 || table_width > 0x7fffffffll / page_size ||
-      queue_size > 0x7fffffffll || tokens > 0x7fffffffll || window > 0x7fffffffll ||
-      sinks > 0x7fffffffll)
+  if (x.tokens > 0 && (!x.slots || !x.positions)) return LILICORR_ERR_INVALID_ARG;
+  if (x.pages_out == x.pages || x.cursor_out == x.cursor) return LILICORR_ERR_INVALID_ARG;
+  if (x.N > kPlanMaxN || x.page_size > 65536 || x.table_width > 0x7fffffffll / x.page_size ||
+      x.queue_size > 0x7fffffffll || x.tokens > 0x7fffffffll || x.window > 0x7fffffffll ||
+      x.sinks > 0x7fffffffll - x.page_size)
     return LILICORR_ERR_UNSUPPORTED;
-  if (!aligned4(lengths) || !aligned4(incoming) || !aligned4(pages) || !aligned4(table) ||
-      !aligned4(queue) || !aligned8(cursor) || !aligned4(pages_out) || !aligned8(cursor_out) ||
-      !aligned4(starts) || !aligned4(totals) || !aligned4(slots) || !aligned4(positions))
+  if (!aligned4(x.lengths) || !aligned4(x.incoming) || !aligned4(x.pages) || !aligned4(x.table) ||
+      !aligned4(x.queue) || !aligned8(x.cursor) || !aligned4(x.pages_out) ||
+      !aligned8(x.cursor_out) || !aligned4(x.starts) || !aligned4(x.totals) || !aligned4(x.slots) ||
+      !aligned4(x.positions))
     return LILICORR_ERR_ALIGNMENT;
   PlanArgs a;
-  a.lengths = lengths; a.incoming = incoming; a.pages = pages;
-  a.table = table; a.queue = queue; a.cursor = cursor;
-  a.N = (int)N; a.P = page_size; a.M = (int)table_width; a.C = (int)queue_size;
-  a.tokens = tokens; a.window = window;
-  a.first = (int)((sinks + page_size - 1) / page_size);
-  a.pages_out = pages_out; a.cursor_out = cursor_out;
-  a.starts = starts; a.totals = totals; a.slots = slots; a.positions = positions;
+  a.lengths = x.lengths; a.incoming = x.incoming; a.pages = x.pages;
+  a.table = x.table; a.queue = x.queue; a.cursor = x.cursor;
+  a.N = (int)x.N; a.P = (int)x.page_size; a.M = (int)x.table_width; a.C = (int)x.queue_size;
+  a.tokens = x.tokens; a.window = x.window;
+  a.first = (int)((x.sinks + x.page_size - 1) / x.page_size);
+  a.pages_out = x.pages_out; a.cursor_out = x.cursor_out;
+  a.starts = x.starts; a.totals = x.totals; a.slots = x.slots; a.positions = x.positions;
   // a workgroup for 256 tokens; a batch without new tokens still has pages to give back
-  int64_t grid = (tokens + kPlanThreads - 1) / kPlanThreads;
-  if (grid < (N + 63) / 64) grid = (N + 63) / 64;
+  int64_t grid = (x.tokens + kPlanThreads - 1) / kPlanThreads;
+  if (grid < (x.N + 63) / 64) grid = (x.N + 63) / 64;
   if (grid > 1024) grid = 1024;
   hipLaunchKernelGGL(page_plan_kernel, dim3((unsigned)grid), dim3(kPlanThreads),
-                     3 * ((size_t)N + 1) * sizeof(int), stream, a);
+                     3 * ((size_t)x.N + 1) * sizeof(int), stream, a);
   return launch_status();
 }
 
-extern "C" lilicorr_status lilicorr_qk_norm_rope(
-    const void* q, int64_t q_stride, int heads, const void* k, int64_t k_stride, const void* v,
-    int64_t v_stride, int64_t tokens, const int32_t* slots, const int32_t* positions,
-    const float* cos_sin, int64_t max_positions, int rot, int interleaved, const float* q_weight,
-    const float* k_weight, float eps, const lilicorr_cache* cache, void* q_out,
-    hipStream_t stream) {
-  if (!cache) return LILICORR_ERR_INVALID_ARG;
-  if (const lilicorr_status s = cache_sizes(*cache)) return s;
-  if (heads < 1 || tokens < 0 || rot < 0 || rot > cache->d || max_positions < 0)
+extern "C" lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_args* args,
+                                                 hipStream_t stream) {
+  if (!args) return LILICORR_ERR_INVALID_ARG;
+  const lilicorr_qk_norm_rope_args& x = *args;
+  const lilicorr_cache& c = x.cache;
+  if (const lilicorr_status s = cache_sizes(c)) return s;
+  if (x.heads < 1 || x.tokens < 0 || x.rot < 0 || x.rot > c.d || x.max_positions < 0)
     return LILICORR_ERR_INVALID_ARG;
-  if (rot > 0 && !cos_sin) return LILICORR_ERR_INVALID_ARG;
-  if (!(eps >= 0.f) || !isfinite(eps)) return LILICORR_ERR_INVALID_ARG;
-  if (q_stride < 0 || k_stride < 0 || v_stride < 0) return LILICORR_ERR_INVALID_ARG;
-  if (rot % 16 || heads > 65535 || tokens > 0x7fffffffll) return LILICORR_ERR_UNSUPPORTED;
-  if (tokens == 0) return LILICORR_OK;
-  if (!q || !k || !v || !slots || !positions || !q_out || !cache->k || !cache->v)
+  if (!(x.eps >= 0.f) || !isfinite(x.eps)) return LILICORR_ERR_INVALID_ARG;
+  if (x.q_stride < 0 || x.k_stride < 0 || x.v_stride < 0) return LILICORR_ERR_INVALID_ARG;
+  if (x.rot % 16 || x.heads > 65535 || x.tokens > 0x7fffffffll) return LILICORR_ERR_UNSUPPORTED;
+  if (!stride_ok(x.q_stride) || !stride_ok(x.k_stride) || !stride_ok(x.v_stride))
+    return LILICORR_ERR_ALIGNMENT;
+  if (x.tokens == 0) return LILICORR_OK;
+  if (!x.q || !x.k || !x.v || !x.slots || !x.positions || !x.q_out || !c.k || !c.v ||
+      (x.rot > 0 && !x.cos_sin))
     return LILICORR_ERR_INVALID_ARG;
   // q rows that are turned in place must be laid out as the output is
-  if (q_out == q && q_stride != (int64_t)heads * cache->d) return LILICORR_ERR_INVALID_ARG;
-  if (!stride_ok(q_stride) || !stride_ok(k_stride) || !stride_ok(v_stride))
-    return LILICORR_ERR_ALIGNMENT;
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) ||
-      !aligned16(cache->k) || !aligned16(cache->v) || (cos_sin && !aligned16(cos_sin)) ||
-      (q_weight && !aligned16(q_weight)) || (k_weight && !aligned16(k_weight)) ||
-      !aligned4(slots) || !aligned4(positions))
+  if (x.q_out == x.q && x.tokens > 1 && x.q_stride != (int64_t)x.heads * c.d)
+    return LILICORR_ERR_INVALID_ARG;
+  if (!aligned16(x.q) || !aligned16(x.k) || !aligned16(x.v) || !aligned16(x.q_out) ||
+      !aligned16(c.k) || !aligned16(c.v) || !aligned16(x.cos_sin) || !aligned16(x.q_weight) ||
+      !aligned16(x.k_weight) || !aligned4(x.slots) || !aligned4(x.positions))
     return LILICORR_ERR_ALIGNMENT;
   RopeArgs a;
-  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
-  a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
-  a.tokens = tokens;
-  a.heads = heads; a.kv_heads = cache->heads; a.d = cache->d; a.rot = rot;
-  a.interleaved = interleaved != 0;
-  a.slots = slots; a.positions = positions; a.cos_sin = cos_sin; a.max_positions = max_positions;
-  a.q_weight = q_weight; a.k_weight = k_weight; a.eps = eps;
-  a.k_cache = (uint16_t*)cache->k; a.v_cache = (uint16_t*)cache->v; a.q_out = (uint16_t*)q_out;
-  a.pages = cache->pages; a.page_stride = cache->page_stride;
-  a.token_stride = cache->token_stride; a.head_stride = cache->head_stride;
-  a.page_size = cache->page_size;
+  a.q = (const uint16_t*)x.q; a.k = (const uint16_t*)x.k; a.v = (const uint16_t*)x.v;
+  a.q_stride = x.q_stride; a.k_stride = x.k_stride; a.v_stride = x.v_stride;
+  a.tokens = x.tokens;
+  a.heads = x.heads; a.kv_heads = c.heads; a.d = c.d; a.rot = x.rot;
+  a.interleaved = x.interleaved != 0;
+  a.slots = x.slots; a.positions = x.positions; a.cos_sin = x.cos_sin;
+  a.max_positions = x.max_positions;
+  a.q_weight = x.q_weight; a.k_weight = x.k_weight; a.eps = x.eps;
+  a.k_cache = (uint16_t*)c.k; a.v_cache = (uint16_t*)c.v; a.q_out = (uint16_t*)x.q_out;
+  a.pages = c.pages; a.page_stride = c.page_stride; a.token_stride = c.token_stride;
+  a.head_stride = c.head_stride;
+  a.page_size = c.page_size;
   // few tokens: their heads spread over more waves
-  a.parts = tokens >= 4096 ? 1 : tokens >= 512 ? 4 : 12;
-  if (cache->dtype == LILICORR_BF16) launch_rope<Bf16>(a, stream);
+  a.parts = x.tokens >= 4096 ? 1 : x.tokens >= 512 ? 4 : 12;
+  if (c.dtype == LILICORR_BF16) launch_rope<Bf16>(a, stream);
   else launch_rope<F16>(a, stream);
   return launch_status();
 }
