@@ -11,39 +11,37 @@
 namespace lilicorr {
 namespace {
 
-constexpr size_t kHeaderBytes = 256;
 constexpr int kTargetItems = 512;  // workgroups that fill the chip: two on each of 256 compute units
+constexpr size_t kLeastBytes = 256;  // of a workspace
 
 // One pass over keys: which tile height, how many tiles and chunks
 struct Pass {
-  int BM, tiles, chunk, chunks;
+  int tiles, chunk, chunks;
   bool spread;
 };
 
 struct Plan {
   bool shared;
+  int BM;
   Pass first, tail;  // the shared keys' pass and the requests' own
   int slots;
   int64_t rows;
-  size_t bytes;
+  size_t bytes;  // of the workspace
 };
 
 int tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
-// keys: the most that a tile sees; stage: the largest stage of the kernels, which chunks are whole
-// multiples of
-Pass make_pass(int64_t rows_each, int64_t tiles, int heads, int64_t keys, int BM) {
+// `share` workgroups for the tiles of all heads, each seeing at most `keys` keys
+Pass make_pass(int64_t tiles, int heads, int64_t keys, double share) {
   Pass p;
-  p.BM = BM;
   p.tiles = (int)tiles;
   constexpr int64_t kLeast = 256;  // keys of a chunk that are worth its partial results
-  const int64_t items = tiles * heads;
-  int64_t chunks = (kTargetItems + items - 1) / items;
+  int64_t chunks = (int64_t)(share / (double)(tiles * heads) + 0.5);
   const int64_t most = (keys + kLeast - 1) / kLeast;
   if (chunks > most) chunks = most;
   if (chunks < 1) chunks = 1;
   int64_t chunk = (keys + chunks - 1) / chunks;
-  chunk = (chunk + 127) / 128 * 128;
+  chunk = (chunk + 127) / 128 * 128;  // whole stages of every kernel
   if (chunk < 128) chunk = 128;
   p.chunk = (int)chunk;
   p.chunks = (int)((keys + chunk - 1) / chunk);
@@ -87,8 +85,9 @@ lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p
   const int64_t max_tokens = a.max_tokens < a.tokens ? a.max_tokens : a.tokens;
   p.shared = shared;
   p.rows = a.tokens * a.heads;
-  const int64_t own = max_tokens * group;
-  const int BM = tile_rows(own);
+  const int64_t own = max_tokens * group, all = a.tokens * group;
+  // one launch has one tile height; where the shared keys are read for all rows together, theirs
+  const int BM = tile_rows(shared ? all : own);
   const int64_t tiles = own <= BM ? a.N : a.tokens * group / BM + a.N;
   int64_t keys = a.table_width * a.cache.page_size;
   if (a.max_length < keys) keys = a.max_length;
@@ -100,67 +99,80 @@ lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p
                          (a.causal && tile_tokens < max_tokens ? tile_tokens : max_tokens);
     if (seen < keys) keys = seen;
   }
-  p.tail = make_pass(own, tiles, a.cache.heads, keys, BM);
+  // the workgroups that fill the chip, dealt out by what the two passes have to do
+  const int64_t shared_tiles = shared ? (all + BM - 1) / BM : 0;
+  const double own_work = (double)tiles * (double)(keys + 128);
+  const double own_share =
+      kTargetItems * own_work / (own_work + (double)shared_tiles * (double)a.shared_length);
+  p.BM = BM;
+  p.tail = make_pass(tiles, a.cache.heads, keys, own_share);
   p.tail.spread = own <= BM;
   p.slots = p.tail.chunks;
   if (shared) {
-    const int64_t all = a.tokens * group;
-    const int BS = tile_rows(all);
-    p.first = make_pass(all, (all + BS - 1) / BS, a.cache.heads, a.shared_length, BS);
+    p.first = make_pass(shared_tiles, a.cache.heads, a.shared_length, kTargetItems - own_share);
     p.first.spread = false;
     p.slots += p.first.chunks;
   }
   const int64_t most_items = 0x7fffffffll / a.cache.heads;
-  if ((int64_t)p.tail.tiles * p.tail.chunks > most_items ||
-      (shared && (int64_t)p.first.tiles * p.first.chunks > most_items))
+  if ((int64_t)p.tail.tiles * p.tail.chunks +
+          (shared ? (int64_t)p.first.tiles * p.first.chunks : 0) > most_items)
     return LILICORR_ERR_UNSUPPORTED;
-  p.bytes = kHeaderBytes;
+  p.bytes = kLeastBytes;
   if (p.slots > 1) p.bytes += (size_t)p.slots * p.rows * (8 + (size_t)a.cache.d * 4);
   return LILICORR_OK;
 }
 
 template <typename C>
-void launch(const AttnArgs& a, int chunks, hipStream_t stream) {
+void launch(const AttnArgs& a, hipStream_t stream) {
   static const hipError_t attr =
       hipFuncSetAttribute(reinterpret_cast<const void*>(attention_kernel<C>),
                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::kLds);
   (void)attr;
-  hipLaunchKernelGGL(attention_kernel<C>, dim3((unsigned)((int64_t)a.tiles * chunks * a.kv_heads)),
+  hipLaunchKernelGGL(attention_kernel<C>, dim3((unsigned)(a.shared.items + a.own.items)),
                      dim3(C::kThreads), C::kLds, stream, a);
 }
 
 template <typename T, bool FULL, int DP>
-void launch_rows(const AttnArgs& a, const Pass& p, hipStream_t stream) {
+void launch_rows(const AttnArgs& a, int BM, hipStream_t stream) {
   if constexpr (DP == 64) {
-    if (p.BM == 32) launch<AttnConfig<T, FULL, 64, 1, 4, 1, 4>>(a, p.chunks, stream);
-    else if (p.BM == 64) launch<AttnConfig<T, FULL, 64, 2, 2, 1, 4>>(a, p.chunks, stream);
-    else launch<AttnConfig<T, FULL, 64, 4, 1, 2, 2>>(a, p.chunks, stream);
+    if (BM == 32) launch<AttnConfig<T, FULL, 64, 1, 4, 1, 4>>(a, stream);
+    else if (BM == 64) launch<AttnConfig<T, FULL, 64, 2, 2, 1, 4>>(a, stream);
+    else launch<AttnConfig<T, FULL, 64, 4, 1, 2, 2>>(a, stream);
   } else if constexpr (DP == 128) {
-    if (p.BM == 32) launch<AttnConfig<T, FULL, 128, 1, 4, 1, 2>>(a, p.chunks, stream);
-    else if (p.BM == 64) launch<AttnConfig<T, FULL, 128, 2, 2, 1, 2>>(a, p.chunks, stream);
-    else launch<AttnConfig<T, FULL, 128, 4, 1, 2, 2>>(a, p.chunks, stream);
+    if (BM == 32) launch<AttnConfig<T, FULL, 128, 1, 4, 1, 2>>(a, stream);
+    else if (BM == 64) launch<AttnConfig<T, FULL, 128, 2, 2, 1, 2>>(a, stream);
+    else launch<AttnConfig<T, FULL, 128, 4, 1, 2, 2>>(a, stream);
   } else {
-    if (p.BM == 32) launch<AttnConfig<T, FULL, 256, 1, 2, 1, 2>>(a, p.chunks, stream);
-    else if (p.BM == 64) launch<AttnConfig<T, FULL, 256, 2, 2, 1, 2>>(a, p.chunks, stream);
-    else launch<AttnConfig<T, FULL, 256, 4, 1, 1, 2>>(a, p.chunks, stream);
+    if (BM == 32) launch<AttnConfig<T, FULL, 256, 1, 2, 1, 2>>(a, stream);
+    else if (BM == 64) launch<AttnConfig<T, FULL, 256, 2, 2, 1, 2>>(a, stream);
+    else launch<AttnConfig<T, FULL, 256, 4, 1, 1, 2>>(a, stream);
   }
 }
 
 template <typename T>
-void launch_pass(AttnArgs a, const Pass& p, hipStream_t stream) {
-  a.tiles = p.tiles;
-  a.chunk = p.chunk;
-  a.spread = p.spread;
-  if (a.d <= 64) {
-    if (a.d == 64) launch_rows<T, true, 64>(a, p, stream);
-    else launch_rows<T, false, 64>(a, p, stream);
-  } else if (a.d <= 128) {
-    if (a.d == 128) launch_rows<T, true, 128>(a, p, stream);
-    else launch_rows<T, false, 128>(a, p, stream);
+void launch_attention(const AttnArgs& a, int BM, hipStream_t stream) {
+  const int d = a.d;
+  if (d <= 64) {
+    if (d == 64) launch_rows<T, true, 64>(a, BM, stream);
+    else launch_rows<T, false, 64>(a, BM, stream);
+  } else if (d <= 128) {
+    if (d == 128) launch_rows<T, true, 128>(a, BM, stream);
+    else launch_rows<T, false, 128>(a, BM, stream);
   } else {
-    if (a.d == 256) launch_rows<T, true, 256>(a, p, stream);
-    else launch_rows<T, false, 256>(a, p, stream);
+    if (d == 256) launch_rows<T, true, 256>(a, BM, stream);
+    else launch_rows<T, false, 256>(a, BM, stream);
   }
+}
+
+AttnPass attn_pass(const Pass& p, int kv_heads, int slot0) {
+  AttnPass r = {};
+  r.tiles = p.tiles;
+  r.chunk = p.chunk;
+  r.most = p.chunk * p.chunks;
+  r.items = p.tiles * p.chunks * kv_heads;
+  r.spread = p.spread;
+  r.slot0 = slot0;
+  return r;
 }
 
 template <typename T, int LPR>
@@ -177,11 +189,10 @@ lilicorr_status run(const lilicorr_attention_args& x, const Plan& p, hipStream_t
   const lilicorr_cache& c = x.cache;
   a.q = (const uint16_t*)x.q; a.k = (const uint16_t*)c.k; a.v = (const uint16_t*)c.v;
   a.out = (uint16_t*)x.out;
-  a.table = x.table; a.starts = x.starts; a.totals = x.totals;
-  a.q_stride = x.q_stride; a.page_stride = c.page_stride; a.token_stride = c.token_stride;
-  a.head_stride = c.head_stride;
+  a.starts = x.starts; a.totals = x.totals;
+  a.q_stride = x.q_stride; a.head_stride = c.head_stride;
   a.rows = p.rows;
-  a.N = (int)x.N; a.table_width = (int)x.table_width; a.pages = (int)c.pages; a.page_size = c.page_size;
+  a.N = (int)x.N; a.pages = (int)c.pages; a.page_size = c.page_size;
   // n / P = (n * mul) >> shift for n < 2^31, mul = floor(2^shift / P) + 1 below 2^32
   int bits = 0;
   while ((1 << bits) < c.page_size) ++bits;
@@ -193,30 +204,28 @@ lilicorr_status run(const lilicorr_attention_args& x, const Plan& p, hipStream_t
   a.page_units = (uint32_t)(c.page_stride / unit);
   a.token_units = (uint32_t)(c.token_stride / unit);
   a.unit_bytes = (uint32_t)(unit * 2);
-  a.window = (int)(x.window < (1 << 30) ? x.window : (1 << 30));
-  a.sinks = (int)(x.sinks < (1 << 30) ? x.sinks : (1 << 30));
-  a.causal = x.causal != 0;
-  a.max_tokens = (int)(x.max_tokens < x.tokens ? x.max_tokens : x.tokens);
-  a.max_length = (int)(x.max_length < (1 << 30) ? x.max_length : (1 << 30));
-  a.split = p.slots > 1;
   a.scale2 = x.scale * 1.4426950408889634f;
-  if (a.split) {
-    unsigned char* w = (unsigned char*)x.workspace + kHeaderBytes;
-    a.part_o = (float*)w;
-    a.part_ml = (f32x2_t*)(w + (size_t)p.slots * p.rows * c.d * 4);
-  }
+  constexpr int64_t kMost = 1 << 30;
+  a.own = attn_pass(p.tail, c.heads, p.shared ? p.first.chunks : 0);
+  a.own.table = x.table;
+  a.own.table_width = (int)x.table_width;
+  a.own.max_tokens = (int)(x.max_tokens < x.tokens ? x.max_tokens : x.tokens);
+  a.own.max_length = (int)(x.max_length < kMost ? x.max_length : kMost);
+  a.own.window = (int)(x.window < kMost ? x.window : kMost);
+  a.own.sinks = (int)(x.sinks < kMost ? x.sinks : kMost);
+  a.own.causal = x.causal != 0;
   if (p.shared) {
-    AttnArgs s = a;
-    s.shared = (int)x.shared_length;
-    s.table = x.shared_table;
-    s.table_width = (int)((x.shared_length + c.page_size - 1) / c.page_size);
-    s.max_length = s.shared;
-    s.max_tokens = a.tokens;
-    s.causal = s.window = s.sinks = 0;
-    launch_pass<T>(s, p.first, stream);
-    a.slot0 = p.first.chunks;
+    a.shared = attn_pass(p.first, c.heads, 0);
+    a.shared.table = x.shared_table;
+    a.shared.table_width = (int)((x.shared_length + c.page_size - 1) / c.page_size);
+    a.shared.shared = a.shared.max_length = (int)x.shared_length;
+    a.shared.max_tokens = a.tokens;
   }
-  launch_pass<T>(a, p.tail, stream);
+  unsigned char* w = (unsigned char*)x.workspace;
+  a.split = p.slots > 1;
+  a.part_o = (float*)w;
+  a.part_ml = (f32x2_t*)(w + (size_t)p.slots * p.rows * c.d * 4);
+  launch_attention<T>(a, p.BM, stream);
   if (a.split) {
     if (c.d <= 64) launch_join<T, 16>(a, p, stream);
     else if (c.d <= 128) launch_join<T, 32>(a, p, stream);

@@ -111,24 +111,35 @@ __device__ __forceinline__ void copy_to_lds(lds_t dst, const unsigned char* src)
   __asm__ volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(at), "v"(src) : "memory");
 }
 
+// One pass over keys: over the requests' own ones, or over the shared ones for every query
+struct AttnPass {
+  const int32_t* table;
+  int table_width;
+  int shared;          // 0, or the length of the shared keys, which this pass is for
+  int tiles, chunk;    // row tiles; keys of a chunk
+  int most;            // keys of all chunks
+  int items;           // tiles * heads * chunks
+  int spread;          // XCDs take runs of items instead of every eighth
+  int slot0;           // slot of chunk 0
+  int max_tokens, max_length;
+  int window, sinks, causal;
+};
+
 struct AttnArgs {
   const uint16_t *q, *k, *v;
   uint16_t* out;
-  float* part_o;   // [slots][tokens * heads][d], where the keys are split
+  float* part_o;     // [slots][tokens * heads][d], where the keys are split
   f32x2_t* part_ml;  // [slots][tokens * heads]: maximum (powers of two) and sum
-  const int32_t *table, *starts, *totals;
-  int64_t q_stride, page_stride, token_stride, head_stride, rows;  // rows = tokens * heads
-  int N, table_width, pages, page_size;
+  const int32_t *starts, *totals;
+  int64_t q_stride, rows;  // rows = tokens * heads
+  int64_t head_stride;
+  int N, pages, page_size;
   uint32_t page_mul, page_shift;  // n / page_size = (n * page_mul) >> page_shift
   int tokens, heads, kv_heads, group, d;
   uint32_t page_units, token_units, unit_bytes;  // page and token strides in a common unit
-  int window, sinks, causal;
-  int max_tokens, max_length;
-  int shared;            // 0, or the length of the shared keys, which this pass is for
-  int tiles, chunk, slot0;  // keys of a chunk; slot of chunk 0
-  int spread;                       // XCDs take runs of items instead of every eighth
-  int split;                        // whether partial results are written
-  float scale2;                     // scale * log2 e
+  int split;     // whether partial results are written, which attention_join_kernel joins
+  float scale2;  // scale * log2 e
+  AttnPass shared, own;
 };
 
 template <typename T_, bool FULL_, int DP_, int WR_, int WK_, int KB_, int NS_>
@@ -157,7 +168,6 @@ struct AttnConfig {
   static constexpr size_t kLds = kFlag + 16;
   static_assert(KB <= 2, "blocks of a stage and wave");
   static_assert(WROWS % RPI == 0 && WROWS <= kWave, "whole copy instructions");
-  static_assert(SK <= kWave || WR == 1, "a wave looks up the pages of what it copies and uses");
 };
 
 // Piece c of row r of a stage lies at place c ^ swizzle(r) of the row. The keys' reads take one piece of 32
@@ -183,9 +193,9 @@ struct Keys {
 // One row by one wave, key by key, in fp32: what a tile falls back to when a value among the keys that
 // not all of its rows see is infinite or NaN. A lane has four elements of the head.
 template <typename T>
-__device__ __forceinline__ void attention_row(const AttnArgs& a, const Keys keys, int start,
-                                                        int pos0, int head, int r, int chunk_no,
-                                                        const uint16_t* kbase, const uint16_t* vbase) {
+__device__ __forceinline__ void attention_row(const AttnArgs& a, const AttnPass& ps, const Keys keys,
+                                             int start, int pos0, int head, int r, int64_t part_row,
+                                             const uint16_t* kbase, const uint16_t* vbase) {
   const int x = lane_id() * 4;
   const bool mine = x < a.d;
   const int tok = r / a.group, p = pos0 + tok, h = head * a.group + (r - tok * a.group);
@@ -200,10 +210,11 @@ __device__ __forceinline__ void attention_row(const AttnArgs& a, const Keys keys
   load(a.q + ((int64_t)start + tok) * a.q_stride + (int64_t)h * a.d, q);
   for (int i = keys.begin; i < keys.end; ++i) {
     const int j = i < keys.ns ? i : i + keys.shift;
-    if ((a.causal && j > p) || (a.window && j <= p - a.window && j >= a.sinks)) continue;
+    if ((ps.causal && j > p) || (ps.window && j <= p - ps.window && j >= ps.sinks)) continue;
     const int e = j / a.page_size, page = keys.table[e];
     if (page < 0 || page >= a.pages) continue;
-    const int64_t at = (int64_t)page * a.page_stride + (int64_t)(j - e * a.page_size) * a.token_stride;
+    const int64_t at = ((int64_t)((uint32_t)page * a.page_units +
+                                  (uint32_t)(j - e * a.page_size) * a.token_units) * a.unit_bytes) >> 1;
     float k[4], v[4];
     load(kbase + at, k);
     load(vbase + at, v);
@@ -216,8 +227,8 @@ __device__ __forceinline__ void attention_row(const AttnArgs& a, const Keys keys
 #pragma unroll
     for (int c = 0; c < 4; ++c) o[c] = o[c] * f + w * v[c];
   }
-  if (a.split) {
-    const int64_t at = (int64_t)(a.slot0 + chunk_no) * a.rows + orow;
+  if (part_row >= 0) {
+    const int64_t at = part_row + orow;
     if (lane_id() == 0) a.part_ml[at] = f32x2_t{m, l};
     if (mine) *reinterpret_cast<f32x4_t*>(a.part_o + at * a.d + x) = f32x4_t{o[0], o[1], o[2], o[3]};
   } else if (mine) {
@@ -228,7 +239,8 @@ __device__ __forceinline__ void attention_row(const AttnArgs& a, const Keys keys
 }
 
 template <typename C>
-__device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item, unsigned char* smem) {
+__device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass& ps, const int item,
+                                               unsigned char* smem) {
   typedef typename C::T T;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = (int)__builtin_amdgcn_readfirstlane(tid >> 6);
@@ -237,23 +249,23 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
 
   // ---- which rows ------------------------------------------------------------------------------
   int it = item;
-  if (a.spread) {
-    const int per = (int)gridDim.x / 8;
+  if (ps.spread) {
+    const int per = ps.items / 8;
     if (it < per * 8) it = (it % 8) * per + it / 8;
   }
   const int head = it % a.kv_heads;
   const int rest = it / a.kv_heads;
-  const int chunk_no = rest / a.tiles;
+  const int chunk_no = rest / ps.tiles;
   // long rows first: with a causal mask and no window the last tiles of a request see most
-  const int tile = a.tiles - 1 - rest % a.tiles;
+  const int tile = ps.tiles - 1 - rest % ps.tiles;
   int n = 0, r0, start = 0, T_all, total;
   auto starts_at = [&](int i) { return min(max(a.starts[i], 0), a.tokens); };
-  if (a.shared) {  // every query, against the shared keys
+  if (ps.shared) {  // every query, against the shared keys
     r0 = tile * C::BM;
     T_all = starts_at(a.N);
-    total = a.shared;
+    total = ps.shared;
   } else {
-    if ((int64_t)a.max_tokens * a.group <= C::BM) {
+    if ((int64_t)ps.max_tokens * a.group <= C::BM) {
       n = tile;
       r0 = 0;
     } else {
@@ -277,7 +289,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
     T_all = starts_at(n + 1) - start;
     total = max(a.totals[n], 0);
   }
-  const int T_n = min(T_all, a.max_tokens);
+  const int T_n = min(T_all, ps.max_tokens);
   if (r0 < 0) return;
   if (r0 >= (int64_t)T_n * a.group) return;
   const int r1 = (int)min((int64_t)T_n * a.group, (int64_t)r0 + C::BM);
@@ -285,26 +297,28 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
 
   // ---- which keys ------------------------------------------------------------------------------
   const int p_lo = pos0 + r0 / a.group, p_hi = pos0 + (r1 - 1) / a.group;
-  int hi = a.causal ? min(total, p_hi + 1) : total;
-  hi = max(min(min(hi, a.max_length), (int)(a.table_width * (int64_t)a.page_size)), 0);
-  const int lo = a.window ? min(max(p_lo - a.window + 1, 0), hi) : 0;
-  const int ns = min(a.sinks, lo);
+  int hi = ps.causal ? min(total, p_hi + 1) : total;
+  hi = max(min(min(hi, ps.max_length), (int)(ps.table_width * (int64_t)a.page_size)), 0);
+  const int lo = ps.window ? min(max(p_lo - ps.window + 1, 0), hi) : 0;
+  const int ns = min(ps.sinks, lo);
   const int shift = lo - ns;
-  const int nv = ns + hi - lo;
-  const int v_begin = chunk_no * a.chunk;
-  const int v_end = (int)min((int64_t)nv, (int64_t)v_begin + a.chunk);
+  const int nv = min(ns + hi - lo, ps.most);
+  const int v_begin = chunk_no * ps.chunk;
+  const int v_end = (int)min((int64_t)nv, (int64_t)v_begin + ps.chunk);
 
   const int row = r0 + wr * 32 + col;  // this lane's row
   const int rowc = min(row, r1 - 1);
   const int tok = rowc / a.group;
   const int64_t orow = ((int64_t)start + tok) * a.heads + head * a.group + (rowc - tok * a.group);
   const int p = pos0 + tok;  // its position: it sees the keys from j_least to j_most, and the sinks
-  const int j_most = a.causal ? p : 0x3fffffff, j_least = a.window ? p - a.window + 1 : -0x3fffffff;
+  const int j_most = ps.causal ? p : 0x3fffffff, j_least = ps.window ? p - ps.window + 1 : -0x3fffffff;
   if (v_begin >= nv && chunk_no > 0) {  // (chunk 0 of a tile without keys writes its zeros below)
     if (wk == 0 && half == 0 && row < r1)
-      a.part_ml[(int64_t)(a.slot0 + chunk_no) * a.rows + orow] = f32x2_t{-__builtin_inff(), 0.f};
+      a.part_ml[(int64_t)(ps.slot0 + chunk_no) * a.rows + orow] = f32x2_t{-__builtin_inff(), 0.f};
     return;
   }
+  // where the chunk's partial results go
+  const int64_t part_row = a.split ? (int64_t)(ps.slot0 + chunk_no) * a.rows : -1;
   // the wave's rows, for the whole block's sake: positions of its first and last
   const int wrow0 = r0 + wr * 32;
   const int wp_lo = pos0 + min(wrow0, r1 - 1) / a.group;
@@ -326,7 +340,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   const uint16_t* kbase = a.k + (int64_t)head * a.head_stride;
   const uint16_t* vbase = a.v + (int64_t)head * a.head_stride;
   const unsigned char *kbytes = (const unsigned char*)kbase, *vbytes = (const unsigned char*)vbase;
-  const int32_t* trow = a.table + (int64_t)n * a.table_width;
+  const int32_t* trow = ps.table + (int64_t)n * ps.table_width;
   // The page numbers of the list's positions, in LDS: the entries of the sinks, then those of the
   // window. A wave keeps kEntries of them, from number x0 on, and fetches the next ones when a stage
   // runs out of them, so that page numbers are not waited for among the copies.
@@ -340,13 +354,19 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   bool absent = false;  // a page among those so far is not there
   auto fetch = [&](int x, int x_last) {
     x0 = x;
+    int page[C::kEntries / kWave];
+    bool gone = false;
 #pragma unroll
     for (int u = 0; u < C::kEntries / kWave; ++u) {
       const int y = min(x + u * kWave + lane, x_last);
-      const int page = trow[y < xs ? y : y - xs + e_lo];
-      absent |= __ballot(page < 0 || page >= a.pages) != 0;
-      *(lds_int_t)(smem + tab + (u * kWave + lane) * 4) = page;
+      page[u] = trow[y < xs ? y : y - xs + e_lo];
     }
+#pragma unroll
+    for (int u = 0; u < C::kEntries / kWave; ++u) {
+      gone |= page[u] < 0 || page[u] >= a.pages;
+      *(lds_int_t)(smem + tab + (u * kWave + lane) * 4) = page[u];
+    }
+    absent |= __ballot(gone) != 0;
   };
   const int x_last = v_end > 0 ? number_of(v_end - 1, entry_of(v_end - 1 < ns ? v_end - 1 : v_end - 1 + shift)) : 0;
   const int my_row = lane / C::CPR, my_pos = lane % C::CPR;
@@ -453,7 +473,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
     }
     here &= bits_below(v_end - v0);
     const bool whole = here == kAll && (v0 >= ns || shift == 0) &&
-                       (!a.causal || j_hi <= wp_lo) && (!a.window || j_lo > wp_hi - a.window);
+                       (!ps.causal || j_hi <= wp_lo) && (!ps.window || j_lo > wp_hi - ps.window);
     // the list's positions v0 .. that this lane's row sees: of the sinks' part keys up to its own, of
     // the window's part its window, and sinks that lie in it
     uint64_t vis = 0;
@@ -461,7 +481,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
       const uint64_t part = bits_below(ns - v0);
       const int w0 = v0 + shift;
       vis = here & ((part & bits_below(j_most + 1 - v0)) |
-                    (~part & bits_below(j_most + 1 - w0) & (bits_from(j_least - w0) | bits_below(a.sinks - w0))));
+                    (~part & bits_below(j_most + 1 - w0) & (bits_from(j_least - w0) | bits_below(ps.sinks - w0))));
       vis >>= 4 * half;
     }
     // Blocks of 32 keys. While one block's powers are taken, the matrix cores have the next block's
@@ -614,7 +634,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   if (*again) {
     const Keys keys = {trow, v_end, v_begin, ns, shift};
     for (int r = r0 + wave; r < r1; r += C::kWaves)
-      attention_row<T>(a, keys, start, pos0, head, r, chunk_no, kbase, vbase);
+      attention_row<T>(a, ps, keys, start, pos0, head, r, part_row, kbase, vbase);
     return;
   }
 
@@ -662,8 +682,8 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
 
   // ---- write ---------------------------------------------------------------------------------------
   if (row >= r1) return;
-  if (a.split) {
-    const int64_t at = (int64_t)(a.slot0 + chunk_no) * a.rows + orow;
+  if (part_row >= 0) {
+    const int64_t at = part_row + orow;
     if (wk == 0 && half == 0) a.part_ml[at] = f32x2_t{mp, l};
     float* po = a.part_o + at * a.d;
 #pragma unroll
@@ -702,11 +722,13 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const int item
   }
 }
 
+// The shared keys' items come first, where there are any, then the requests' own.
 template <typename C>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::DP > 128 ? 1 : 2, C::DP > 128 ? 1 : 2)))
 void attention_kernel(AttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char attn_smem[];
-  attention_tile<C>(a, (int)blockIdx.x, attn_smem);
+  const int item = (int)blockIdx.x - a.shared.items;
+  attention_tile<C>(a, item < 0 ? a.shared : a.own, item < 0 ? (int)blockIdx.x : item, attn_smem);
 }
 
 // Joins the slots of every row in their order, a wave a row: maxima and sums one lane a slot, then the
@@ -721,39 +743,49 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(
   const int lane = lane_id();
   const int64_t row = (int64_t)blockIdx.x * (kJoinThreads / kWave) + threadIdx.x / kWave;
   const int x = (lane % LPR) * 4;
-  if (row >= rows || row >= (int64_t)min(max(starts[N], 0), tokens) * heads) return;
+  if (row >= rows) return;
+  const int64_t used = (int64_t)min(max(starts[N], 0), tokens) * heads;
   float top = -__builtin_inff(), l = 0.f;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < slots; s0 += kWave) {
+    const int here = min(slots - s0, kWave);
+    constexpr int kBatch = 8;
+    f32x4_t v[kBatch];
+    // a slot that saw nothing holds no output: read all the same, beside its sum, and not used
+    auto load = [&](int b) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int s = b + u * kAtOnce + lane / LPR;
+        v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (s < here && x < d)
+          v[u] = *reinterpret_cast<const f32x4_t*>(part_o + ((s0 + s) * rows + row) * d + x);
+      }
+    };
     f32x2_t ml = {-__builtin_inff(), 0.f};
-    if (s0 + lane < slots) ml = part_ml[(s0 + lane) * rows + row];
+    if (lane < here) ml = part_ml[(s0 + lane) * rows + row];
+    load(0);
     const float grown = fmaxf(top, wave_max_dpp(ml[0]));
     const float f0 = top == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(top - grown);
-    // a slot that saw nothing has the sum 0; a NaN stays one
+    // the sum of a slot that saw nothing is 0; a NaN stays one
     const float f = ml[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[0] - grown);
     const bool saw = ml[1] != 0.f;
     top = grown;
     l = l * f0 + wave_sum_dpp(saw ? f * ml[1] : 0.f);
     o *= f0;
     const uint64_t which = __ballot(saw);
-    const int here = min(slots - s0, kWave);
-    constexpr int kBatch = 8;
     for (int b = 0; b < here; b += kBatch * kAtOnce) {
-      f32x4_t v[kBatch];
-      float w[kBatch];
+      if (b) load(b);
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         const int s = b + u * kAtOnce + lane / LPR;
-        const bool on = s < here && ((which >> (s & 63)) & 1) && x < d;
-        w[u] = __shfl(f, s & 63, kWave);
-        v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (on) v[u] = *reinterpret_cast<const f32x4_t*>(part_o + ((s0 + s) * rows + row) * d + x);
-        if (!on) w[u] = 0.f;
-      }
+        const bool on = s < here && ((which >> (s & 63)) & 1);
+        const float w = __shfl(f, s & 63, kWave);
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) o += w[u] * v[u];
+        for (int e = 0; e < 4; ++e) o[e] += on ? w * v[u][e] : 0.f;
+      }
     }
   }
+  if (row >= used) return;
 #pragma unroll
   for (int m = LPR; m < kWave; m <<= 1)
 #pragma unroll
