@@ -11,7 +11,6 @@
 namespace lilicorr {
 namespace {
 
-constexpr int kTargetItems = 512;  // workgroups that fill the chip: two on each of 256 compute units
 constexpr size_t kLeastBytes = 256;  // of a workspace
 
 // One pass over keys: which tile height, how many tiles and chunks
@@ -31,22 +30,56 @@ struct Plan {
 
 int tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
-// `share` workgroups for the tiles of all heads, each seeing at most `keys` keys
-Pass make_pass(int64_t tiles, int heads, int64_t keys, double share) {
-  Pass p;
-  p.tiles = (int)tiles;
-  constexpr int64_t kLeast = 256;  // keys of a chunk that are worth its partial results
-  int64_t chunks = (int64_t)(share / (double)(tiles * heads) + 0.5);
-  const int64_t most = (keys + kLeast - 1) / kLeast;
-  if (chunks > most) chunks = most;
-  if (chunks < 1) chunks = 1;
-  int64_t chunk = (keys + chunks - 1) / chunks;
-  chunk = (chunk + 127) / 128 * 128;  // whole stages of every kernel
-  if (chunk < 128) chunk = 128;
-  p.chunk = (int)chunk;
-  p.chunks = (int)((keys + chunk - 1) / chunk);
-  if (p.chunks < 1) p.chunks = 1;
-  return p;
+// Keys of a kernel's stage, and its workgroups that run at once on 256 compute units (LDS and, for 128
+// rows, registers)
+struct Fit {
+  int stage, slots;
+};
+Fit kernel_fit(int d, int BM) {
+  const int stage = d <= 128 ? (BM == 32 ? 128 : 64) : (BM == 128 ? 32 : 64);
+  const int each = d <= 64 ? (BM == 32 ? 1 : BM == 64 ? 2 : 3) : d <= 128 ? (BM == 32 ? 1 : 2) : 1;
+  return {stage, 256 * each};
+}
+
+// A pass's row tiles (of all heads) and the stages of keys that a tile sees at most
+struct Work {
+  int64_t items, stages;
+};
+
+// How many stages a chunk has, for both passes: the least of an estimate in stages' times. A workgroup
+// begins and ends for about three (page numbers, queries, first copies; output). As long as all run at
+// once the longest one counts, else also the work of all over the workgroups that run at once, and half
+// of a last one. Split keys add the join's launch (two and a half) and fp32 partial outputs that are written
+// and read again, at 5 TB/s against 1.5 us a stage.
+int64_t chunk_stages(const Work& shared, const Work& own, int slots, int64_t out_elements) {
+  const int64_t longest = shared.stages > own.stages ? shared.stages : own.stages;
+  int64_t best = longest, last = 0;
+  double least = 0;
+  for (int64_t k = 1; k <= 64; ++k) {
+    const int64_t s = (longest + k - 1) / k;
+    if (s == last) continue;
+    last = s;
+    const int64_t cs = (shared.stages + s - 1) / s, co = (own.stages + s - 1) / s;
+    const double groups = (double)shared.items * cs + (double)own.items * co;
+    double t = s + 3;
+    if (groups > slots) {
+      const double all =
+          ((double)shared.items * shared.stages + (double)own.items * own.stages + 3 * groups) / slots;
+      t = (all > t ? all : t) + 0.5 * (s < own.stages ? s : own.stages) + 3;
+    }
+    if (cs + co > 1) t += 2.5 + (double)(cs + co) * out_elements * 8 / 5e6 / 1.5;
+    if (k == 1 || t < least) {
+      least = t;
+      best = s;
+    }
+    if (s == 1) break;
+  }
+  return best;
+}
+
+Pass make_pass(int64_t tiles, int64_t stages, int64_t chunk, int stage, bool spread) {
+  const int64_t chunks = (stages + chunk - 1) / chunk;
+  return {(int)tiles, (int)(chunk * stage), (int)(chunks < 1 ? 1 : chunks), spread};
 }
 
 // the largest unit that page and token strides are whole multiples of: the kernels count offsets in it
@@ -99,18 +132,20 @@ lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p
                          (a.causal && tile_tokens < max_tokens ? tile_tokens : max_tokens);
     if (seen < keys) keys = seen;
   }
-  // the workgroups that fill the chip, dealt out by what the two passes have to do
   const int64_t shared_tiles = shared ? (all + BM - 1) / BM : 0;
-  const double own_work = (double)tiles * (double)(keys + 128);
-  const double own_share =
-      kTargetItems * own_work / (own_work + (double)shared_tiles * (double)a.shared_length);
+  const Fit fit = kernel_fit(a.cache.d, BM);
+  const auto stages = [&](int64_t k) { return k > 0 ? (k + fit.stage - 1) / fit.stage : 1; };
+  const Work shared_work = {shared_tiles * a.cache.heads, shared ? stages(a.shared_length) : 0};
+  const Work own_work = {tiles * a.cache.heads, stages(keys)};
+  const int64_t chunk = chunk_stages(shared_work, own_work, fit.slots, p.rows * a.cache.d);
   p.BM = BM;
-  p.tail = make_pass(tiles, a.cache.heads, keys, own_share);
-  p.tail.spread = own <= BM;
+  // where every key is read once, runs of items keep a request's heads on one XCD (their tokens lie side
+  // by side, and eight XCDs with a head each would use an eighth of every L2: 825 against 1068 us for 256
+  // tokens); tiles that share keys find them in the L2 of their head's XCD (prefill 664 against 772 us)
+  p.tail = make_pass(tiles, own_work.stages, chunk, fit.stage, own <= BM);
   p.slots = p.tail.chunks;
   if (shared) {
-    p.first = make_pass(shared_tiles, a.cache.heads, a.shared_length, kTargetItems - own_share);
-    p.first.spread = false;
+    p.first = make_pass(shared_tiles, shared_work.stages, chunk, fit.stage, false);
     p.slots += p.first.chunks;
   }
   const int64_t most_items = 0x7fffffffll / a.cache.heads;
@@ -132,36 +167,36 @@ void launch(const AttnArgs& a, hipStream_t stream) {
                      dim3(C::kThreads), C::kLds, stream, a);
 }
 
-template <typename T, bool FULL, int DP>
+// The kernels of a width: waves of rows x waves of keys, 32-key blocks a wave and stage, stages of the
+// ring. Few rows: four waves share the keys and each keeps its own ring; more: barriers, 64 keys a
+// stage, and a ring of two so that two workgroups share a compute unit (a ring of four with one: 302
+// against 188 us for 64 blocks of 16 tokens behind 4096 keys).
+template <typename T, bool FULL, int D>
 void launch_rows(const AttnArgs& a, int BM, hipStream_t stream) {
-  if constexpr (DP == 64) {
-    if (BM == 32) launch<AttnConfig<T, FULL, 64, 1, 4, 1, 4>>(a, stream);
-    else if (BM == 64) launch<AttnConfig<T, FULL, 64, 2, 2, 1, 4>>(a, stream);
-    else launch<AttnConfig<T, FULL, 64, 4, 1, 2, 2>>(a, stream);
-  } else if constexpr (DP == 128) {
-    if (BM == 32) launch<AttnConfig<T, FULL, 128, 1, 4, 1, 2>>(a, stream);
-    else if (BM == 64) launch<AttnConfig<T, FULL, 128, 2, 2, 1, 2>>(a, stream);
-    else launch<AttnConfig<T, FULL, 128, 4, 1, 2, 2>>(a, stream);
+  if constexpr (D <= 64) {
+    if (BM == 32) launch<AttnConfig<T, FULL, D, 1, 4, 1, 4>>(a, stream);
+    else if (BM == 64) launch<AttnConfig<T, FULL, D, 2, 2, 1, 4>>(a, stream);
+    else launch<AttnConfig<T, FULL, D, 4, 1, 2, 2>>(a, stream);
+  } else if constexpr (D <= 128) {
+    if (BM == 32) launch<AttnConfig<T, FULL, D, 1, 4, 1, 2>>(a, stream);
+    else if (BM == 64) launch<AttnConfig<T, FULL, D, 2, 2, 1, 2>>(a, stream);
+    else launch<AttnConfig<T, FULL, D, 4, 1, 2, 2>>(a, stream);
   } else {
-    if (BM == 32) launch<AttnConfig<T, FULL, 256, 1, 2, 1, 2>>(a, stream);
-    else if (BM == 64) launch<AttnConfig<T, FULL, 256, 2, 2, 1, 2>>(a, stream);
-    else launch<AttnConfig<T, FULL, 256, 4, 1, 1, 2>>(a, stream);
+    if (BM == 32) launch<AttnConfig<T, FULL, D, 1, 2, 1, 2>>(a, stream);
+    else if (BM == 64) launch<AttnConfig<T, FULL, D, 2, 2, 1, 2>>(a, stream);
+    else launch<AttnConfig<T, FULL, D, 4, 1, 1, 2>>(a, stream);
   }
 }
 
 template <typename T>
 void launch_attention(const AttnArgs& a, int BM, hipStream_t stream) {
-  const int d = a.d;
-  if (d <= 64) {
-    if (d == 64) launch_rows<T, true, 64>(a, BM, stream);
-    else launch_rows<T, false, 64>(a, BM, stream);
-  } else if (d <= 128) {
-    if (d == 128) launch_rows<T, true, 128>(a, BM, stream);
-    else launch_rows<T, false, 128>(a, BM, stream);
-  } else {
-    if (d == 256) launch_rows<T, true, 256>(a, BM, stream);
-    else launch_rows<T, false, 256>(a, BM, stream);
-  }
+  if (a.d == 64) launch_rows<T, true, 64>(a, BM, stream);
+  else if (a.d < 64) launch_rows<T, false, 64>(a, BM, stream);
+  else if (a.d <= 96) launch_rows<T, false, 96>(a, BM, stream);
+  else if (a.d == 128) launch_rows<T, true, 128>(a, BM, stream);
+  else if (a.d < 128) launch_rows<T, false, 128>(a, BM, stream);
+  else if (a.d == 256) launch_rows<T, true, 256>(a, BM, stream);
+  else launch_rows<T, false, 256>(a, BM, stream);
 }
 
 AttnPass attn_pass(const Pass& p, int kv_heads, int slot0) {

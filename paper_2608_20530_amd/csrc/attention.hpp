@@ -142,11 +142,13 @@ struct AttnArgs {
   AttnPass shared, own;
 };
 
-template <typename T_, bool FULL_, int DP_, int WR_, int WK_, int KB_, int NS_>
+// heads of D elements (FULL) or fewer, in LDS rows of 64, 128 or 256
+template <typename T_, bool FULL_, int D_, int WR_, int WK_, int KB_, int NS_>
 struct AttnConfig {
-  static constexpr bool FULL = FULL_;              // heads of DP elements, not fewer
+  static constexpr bool FULL = FULL_;
+  static constexpr int D = D_, DP = D <= 64 ? 64 : D <= 128 ? 128 : 256;
   typedef T_ T;
-  static constexpr int DP = DP_, WR = WR_, WK = WK_, KB = KB_, NS = NS_;
+  static constexpr int WR = WR_, WK = WK_, KB = KB_, NS = NS_;
   static constexpr int kWaves = WR * WK, kThreads = kWaves * kWave;
   static constexpr int BM = 32 * WR;               // rows of a tile
   static constexpr int SK = 32 * KB * WK;          // keys of a stage
@@ -155,11 +157,11 @@ struct AttnConfig {
   static constexpr int RPI = kWave / CPR;          // rows that one copy instruction moves
   static constexpr int WROWS = SK / kWaves;        // rows of a stage that a wave copies
   static constexpr int IPW = WROWS / RPI;          // copy instructions for them, keys or values
-  static constexpr int ND = DP / 32;               // output tiles
+  static constexpr int ND = D / 32;                // output tiles
   static constexpr int LOOK = SK < kWave ? SK : kWave;  // keys whose page a wave looks up
   static constexpr bool kOwn = WR == 1;            // a wave copies just the keys that it uses
   static constexpr uint32_t kTile = SK * RB, kStage = 2 * kTile, kRing = NS * kStage;
-  static constexpr uint32_t kMerge = kWaves * 32 * DP * 4 + kWaves * kWave * 8;
+  static constexpr uint32_t kMerge = kWaves * 32 * D * 4 + kWaves * kWave * 8;
   // the ring, which the join of the waves uses again; each wave's part of the page table; the word
   // that calls for another try
   static constexpr uint32_t kPages = WK > 1 && kMerge > kRing ? kMerge : kRing;
@@ -325,12 +327,12 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
   const int wp_hi = pos0 + min(wrow0 + 31, r1 - 1) / a.group;
 
   // ---- queries: the second operand of the scores' product ---------------------------------------
-  u32x4_t q[C::DP / 16];
+  u32x4_t q[C::D / 16];
   {
     const uint16_t* qp = a.q + ((int64_t)start + tok) * a.q_stride +
                          (int64_t)(head * a.group + (rowc - tok * a.group)) * a.d;
 #pragma unroll
-    for (int i = 0; i < C::DP / 16; ++i) {
+    for (int i = 0; i < C::D / 16; ++i) {
       const int c = (2 * i + half) * 8;
       q[i] = c < a.d ? *reinterpret_cast<const u32x4_t*>(qp + c) : u32x4_t{0, 0, 0, 0};
     }
@@ -487,7 +489,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
     // Blocks of 32 keys. While one block's powers are taken, the matrix cores have the next block's
     // scores or the last one's output to do: the two are laid out in steps of one matrix instruction
     // each, with operands read three steps ahead, and the scheduler is held to that.
-    constexpr int kQK = C::DP / 16, kPV = 2 * C::ND;  // steps of a block
+    constexpr int kQK = C::D / 16, kPV = 2 * C::ND;  // steps of a block
     f32x16_t sc[C::KB];
     u32x4_t pf[C::KB * 2], kf[4], vf[4];
     auto load_k = [&](int x) {  // operand x % kQK of block x / kQK
@@ -520,9 +522,9 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
       o[i % C::ND] = mfma<T>(vf[(b * kPV + i) & 3], pf[2 * b + i / C::ND], o[i % C::ND]);
     };
     float ms = 0.f;
-    auto power_step = [&](int b, int e0, int n) {
+    auto power_step = [&](int b, int e0, int e1) {
 #pragma unroll
-      for (int e = e0; e < e0 + n; ++e) {
+      for (int e = e0; e < e1; ++e) {
         sc[b][e] = __builtin_amdgcn_exp2f(fmaf(sc[b][e], a.scale2, -ms));
         if (e & 1) {
           uint32_t w = T::pack(sc[b][e - 1], sc[b][e]);
@@ -584,14 +586,14 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
 #pragma unroll
         for (int i = 0; i < kQK; ++i) {
           score_step(b + 1, i);
-          power_step(b, i * (16 / kQK), 16 / kQK);
+          power_step(b, i * 16 / kQK, (i + 1) * 16 / kQK);
           __builtin_amdgcn_sched_barrier(0);
         }
       } else if (b > 0) {
 #pragma unroll
         for (int i = 0; i < kPV; ++i) {
           output_step(b - 1, i);
-          power_step(b, i * (16 / kPV), 16 / kPV);
+          power_step(b, i * 16 / kPV, (i + 1) * 16 / kPV);
           __builtin_amdgcn_sched_barrier(0);
         }
       } else {
@@ -642,7 +644,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
   l = cross_sum(l);
   float mp = m * a.scale2;  // in powers of two
   if constexpr (C::WK > 1) {
-    constexpr uint32_t kMl = C::kWaves * 32 * C::DP * 4;
+    constexpr uint32_t kMl = C::kWaves * 32 * C::D * 4;
 #pragma unroll
     for (int t = 0; t < C::ND; ++t)
 #pragma unroll
