@@ -542,8 +542,9 @@ typedef struct {
  *   (2 i, 2 i + 1) when `interleaved`.
  * All of it in fp32 from the stored values, rounded once (nearest, ties to even) at the end. q goes to
  * q_out, k and (as it is) v to the cache at slots[t]; a token with slots[t] outside the cache
- * (-1: no page) is not written there. A position outside [0, max_positions) gives zeros in q_out and
- * no cache write (the rows past the last token of lilicorr_page_plan).
+ * (-1: no page) is not written there. A position below 0 (the rows past the last token of
+ * lilicorr_page_plan) or, with a rotation, of max_positions or more gives zeros in q_out and no cache
+ * write.
  *   q [tokens][heads][d], k, v [tokens][cache heads][d] of the cache's dtype; q_stride, k_stride,
  *   v_stride elements from token to token (multiples of 8: views of one projection's output fit).
  *   q_weight, k_weight [d] fp32 or NULL; cos_sin [max_positions][rot] fp32, rot / 2 cosines and then
@@ -580,11 +581,14 @@ lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_args *args, hi
  * product, and the output once more. The result does not depend on what else runs, and is the same
  * on every call with the same arguments.
  *   max_tokens, max_length   upper bounds of T and totals that the host knows (they choose tiles and
- *       how far the key axis is split). Queries and keys past them are not computed or seen.
- *   workspace   device scratch of the size the query gives, caller-owned, zero-filled once before its
- *       first use; every call leaves it ready for the next. Calls sharing it must not overlap.
- * Limits: heads a multiple of cache heads; tokens * heads < 2^31; page_size * table_width < 2^31;
- * N < 2^24; scale > 0 and finite. out must not overlap q.
+ *       how far the key axis is split). Keys past them are not seen; the output of queries past them,
+ *       and of rows past starts[N], has no meaning (zeros, what it held, or anything else).
+ *   workspace   device scratch of the size the query gives, caller-owned; what it holds before or after
+ *       a call does not matter. Calls sharing it must not overlap.
+ * Limits: heads a multiple of cache heads, at most 65535; tokens * heads, page_size * table_width and
+ * shared_length at most 2^30; N at most 2^20; every element of the cache less than
+ * 2^32 * gcd(page_stride, token_stride) elements from its start; scale > 0 and finite. out must not
+ * overlap q.
  */
 typedef struct {
     const void *q;                  /* [tokens][heads][d] of the cache's dtype */

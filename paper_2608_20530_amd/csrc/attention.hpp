@@ -21,8 +21,9 @@
 //
 // Softmax: running maximum and sum in fp32. The accumulated output is rescaled only when a
 // row's maximum has grown by more than 2^8 over the one that its powers are taken against (they
-// are then at most 2^8; fp32 sums and either 16-bit type hold that). Probabilities are rounded to
-// the cache's type for the matrix cores, and the sum (fp32) is of the rounded ones, as the output is.
+// are then at most 2^8; fp32 sums and bf16 hold that, and fp16 holds them times 2^7, which it is given).
+// Probabilities are rounded to the cache's type for the matrix cores, and the sum (fp32) is of the rounded
+// ones, as the output is.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -37,10 +38,8 @@ namespace {
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void* lds_void_t;
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
 typedef __attribute__((address_space(3))) u32x4_t* lds_u32x4_t;
-typedef __attribute__((address_space(3))) u32x2_t* lds_u32x2_t;
 typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4_t;
 typedef __attribute__((address_space(3))) float* lds_float_t;
 typedef __attribute__((address_space(3))) int* lds_int_t;
@@ -48,6 +47,12 @@ typedef __attribute__((address_space(3))) unsigned char* lds_t;
 
 constexpr int kWaitLoads = 0x0f70;  // s_waitcnt vmcnt(0) alone
 constexpr float kRescale = 8.f;  // growth of the maximum, in powers of two, that is let pass
+// The power that the maximum's probability gets: fp16 ends at 2^16, and its steps of 2^-24 would lose a long
+// run of small probabilities beside one of 1
+template <typename T>
+constexpr float kLift = 0.f;
+template <>
+constexpr float kLift<F16> = 7.f;
 
 template <typename T>
 __device__ __forceinline__ f32x16_t mfma(const u32x4_t& a, const u32x4_t& b, const f32x16_t& c);
@@ -581,7 +586,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
         load_v(2);
       }
       maximum(b);
-      ms = m == -__builtin_inff() ? 0.f : m * a.scale2;
+      ms = m == -__builtin_inff() ? 0.f : m * a.scale2 - kLift<T>;
       if (b + 1 < C::KB) {
 #pragma unroll
         for (int i = 0; i < kQK; ++i) {
@@ -642,7 +647,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
 
   // ---- join the waves that shared the keys ---------------------------------------------------------
   l = cross_sum(l);
-  float mp = m * a.scale2;  // in powers of two
+  float mp = m * a.scale2 - kLift<T>;  // in powers of two
   if constexpr (C::WK > 1) {
     constexpr uint32_t kMl = C::kWaves * 32 * C::D * 4;
 #pragma unroll

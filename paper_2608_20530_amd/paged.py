@@ -262,7 +262,7 @@ def _workspace(name, q, k_cache, table, shared_length, window, sinks, causal, ma
         max_tokens, max_length))
     if need == 0:
         raise LilicorrError(f"{name} does not support these sizes")
-    return torch.zeros(need, dtype=torch.uint8, device=q.device)
+    return torch.empty(need, dtype=torch.uint8, device=q.device)
 
 
 def _attend(name, q, k_cache, v_cache, shared_table, shared_length, table, starts, totals, window, sinks,
@@ -287,7 +287,7 @@ def window_attention_workspace(q: torch.Tensor, k_cache: torch.Tensor, table: to
                                window: int = 0, sinks: int = 0, causal: bool = True,
                                max_tokens: int | None = None,
                                max_length: int | None = None) -> torch.Tensor:
-    """A zero-filled workspace for window_attention calls of these sizes (kept ready by the calls)."""
+    """A workspace for window_attention calls of these sizes, whose content does not matter."""
     return _workspace("lilicorr_window_attention", q, k_cache, table, 0, window, sinks, causal,
                       max_tokens, max_length)
 
@@ -309,7 +309,7 @@ def prefix_attention_workspace(q: torch.Tensor, k_cache: torch.Tensor, table: to
                                shared_length: int, *, causal: bool = True,
                                max_tokens: int | None = None,
                                max_length: int | None = None) -> torch.Tensor:
-    """A zero-filled workspace for prefix_attention calls of these sizes (kept ready by the calls)."""
+    """A workspace for prefix_attention calls of these sizes, whose content does not matter."""
     return _workspace("lilicorr_prefix_attention", q, k_cache, table, shared_length, 0, 0, causal,
                       max_tokens, max_length)
 

@@ -450,3 +450,58 @@ def test_attention_long_offsets(lib):
     y = dict(x, k_cache=k, v_cache=v, table=torch.full_like(x["table"], -1))
     y["table"][0, :6] = i32(far)
     _check(x, _attend(lib, y), want)
+
+
+@pytest.mark.parametrize("less", [12.3, 16.6, 20.4, 21.6, 23.7])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attention_many_small_probabilities(lib, less, dtype):
+    """One key whose score stands above 65535 equal ones by a factor of 2^less in the powers, with the same
+    value as theirs or none: the small ones must count as much as their number makes them. Many requests
+    with the same pages, so that the keys are split little. Relative errors: u for the output; u for the
+    rounded probabilities, or 2^(less - 32) where a type with steps of 2^-24 holds powers of up to 2^7; 1e-4
+    for the scores (at most 24, in powers of two) and sums."""
+    N, n, d, page = 1024, 1 << 16, 64, 64
+    k = torch.zeros(n // page, page, 1, d, dtype=dtype, device="cuda")
+    v = torch.ones_like(k)
+    q = torch.zeros(N, 1, d, dtype=dtype, device="cuda")
+    q[:, 0, 3] = 1.0
+    k[700, 41, 0, 3] = 1.0
+    table = torch.arange(n // page, dtype=torch.int32, device="cuda").repeat(N, 1)
+    small = (n - 1) * 2.0 ** -less
+    rel = U[dtype] + max(U[dtype], 2.0 ** (less - 32) if dtype is torch.float16 else 0.0) + 1e-4
+    for value in (0.0, 1.0):
+        v[700, 41] = value
+        o = lib.window_attention(q, k, v, table, i32(range(N + 1)), i32([n] * N), max_tokens=1,
+                                 scale=less * float(np.log(2.0)))
+        want = (small + value) / (small + 1.0)
+        assert (o.double() - want).abs().max().item() <= rel * want + TINY[dtype]
+
+
+def test_calls_in_a_graph(lib):
+    """Captured once and replayed with other inputs, with eager work between the replays: the same bits as
+    the eager calls on the same inputs. The attentions split their keys, so the join is recorded too."""
+    new, ctx, shared = [16, 1, 7, 16], [900, 700, 0, 333], 650
+    x = _attention_inputs(new, ctx, 8, 2, 128, 16, torch.bfloat16, seed=5)
+    y = _attention_inputs(new, ctx, 8, 2, 128, 16, torch.bfloat16, shared=shared, seed=6)
+    q, k, v, slots, positions, cs, kc, vc, w = _rope_inputs(40, 8, 2, 128, 128, torch.bfloat16)
+    moved = (x["q"], y["q"], q, k, v, slots)
+    keep, totals = [t.clone() for t in moved], x["totals"].clone()
+
+    def calls():
+        a = lib.qk_norm_rope(q, k, v, slots, positions, cs, kc, vc, q_weight=w[0], k_weight=w[1])
+        return a, kc.clone(), _attend(lib, x, window=300, sinks=3), _attend(lib, y, shared=shared)
+
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = calls()
+    for replay in range(4):
+        for t, t0 in zip(moved, keep):
+            t.copy_(t0.roll(replay, 0))
+        x["totals"].copy_(totals - replay)
+        graph.replay()
+        torch.cuda.synchronize()
+        first = [t.clone() for t in got]
+        for a, b in zip(first, calls()):
+            assert torch.equal(a, b), replay
