@@ -730,6 +730,17 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
 }
 
 // The shared keys' items come first, where there are any, then the requests' own.
+//
+// What bounds it (32 heads over 8 key heads of 128, bf16). Few rows a request: reading the cache, once 256
+// workgroups are there to read it; 765 us for 256 requests of one token and 100 to 8100 keys (5.65 TB/s),
+// 195 us for 64 blocks of 16 behind windows of 4096 (5.2 TB/s). One request: a chain of dependent loads
+// (lengths, page numbers, first keys: 2.9, 1.4 and 2 to 5 us cold), 10 us for one token behind a window of
+// 4096. Many rows: instruction issue; 575 to 615 us (895 to 957 TFLOP/s) for 8192 tokens behind windows of
+// 4096, where matrix instructions run 43% of the time and about 230 vector instructions for 64 keys and 32
+// rows want the same issue slots. What 64 keys of a wave cost there, found by leaving a part out: powers 65 us,
+// copies 87, edges of masks 26, the test of the maximum 17, page numbers 10. Two waves a SIMD need at most
+// 256 registers; tiles of 256 rows in eight waves take 650 us, deeper operand rings and wave priorities
+// gain nothing.
 template <typename C>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::DP > 128 ? 1 : 2, C::DP > 128 ? 1 : 2)))
 void attention_kernel(AttnArgs a) {
@@ -740,6 +751,9 @@ void attention_kernel(AttnArgs a) {
 
 // Joins the slots of every row in their order, a wave a row: maxima and sums one lane a slot, then the
 // partial outputs in 16 bytes a lane, LPR lanes a slot and 64 / LPR slots at once.
+// Its first outputs are asked for beside the sums, so that it takes one round trip: 3.5 us for one token behind
+// a window of 4096, 20 us (bytes) for 32768 rows. A kernel of its own: joined by the last workgroup to arrive, one
+// token took 25 us against 16 (the counter's round trips come after the outputs').
 constexpr int kJoinThreads = 256;
 template <typename T, int LPR>
 __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(

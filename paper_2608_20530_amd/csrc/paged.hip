@@ -20,6 +20,7 @@ namespace {
 // the same call: entries [end, end + take) of a table row and ring places from the tail on are
 // written, entries below end and places from the head on are read. Bound by latency: one round trip
 // for the lengths, the sums in LDS, a search of log2 N LDS reads, one round trip for the page.
+// 4.3 us for one request and a block of 16, 6.6 us for 256 requests and 16384 tokens.
 constexpr int kPlanThreads = 256;
 constexpr int kPlanMaxN = 4096;
 
@@ -199,7 +200,9 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a) {
 // share of heads: the token's cosines and sines, its slot and the norm weights stay in registers. A
 // lane needs its partner's elements of the pairs (i, i + rot / 2): rot is a multiple of 16, so the
 // partner holds them at the same place and four 32-bit shuffles bring them. Bound by HBM: each
-// element read once and written once.
+// element read once and written once (85 us for 16381 tokens of 32 + 2 x 8 heads of 128, 4.8 TB/s; a large
+// copy reaches 5.06). One token is bound by latency, 3.3 us: everything that it needs is asked for in wide
+// loads that do not wait for one another (5.9 with the weights and angles loaded one by one).
 constexpr int kRopeThreads = 256;
 
 struct RopeArgs {
@@ -232,6 +235,18 @@ __device__ __forceinline__ float head_sum(float v) {
   return v;
 }
 
+// COUNT floats from a 16-byte aligned place
+template <int COUNT>
+__device__ __forceinline__ void load_floats(const float* from, float (&to)[8]) {
+  typedef float f32x4_t __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int i = 0; i < COUNT; i += 4) {
+    const f32x4_t t = *reinterpret_cast<const f32x4_t*>(from + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[i + e] = t[e];
+  }
+}
+
 // one lane's part of a head: weights of its own elements and of its partner's, cosines and sines of
 // its pairs
 struct RopeLane {
@@ -257,7 +272,7 @@ __device__ __forceinline__ u32x4_t norm_turn(const u32x4_t& w, bool norm, const 
 #pragma unroll
     for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
     s = head_sum<LPH>(s);
-    inv = 1.f / sqrtf(s / (float)d + eps);
+    inv = rsqrtf(s * (1.f / (float)d) + eps);
   }
   float y[8];
 #pragma unroll
@@ -310,13 +325,15 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
   const int po = a.interleaved || !r.turned ? e0 : (r.upper ? e0 - half : e0 + half);
   r.partner = g * LPH + po / 8;
   const bool norm_q = a.q_weight != nullptr, norm_k = a.k_weight != nullptr;
+  // (lanes that hold nothing read the first ones)
   float qw[8], qp[8], kw[8], kp[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    qw[i] = norm_q && mine ? a.q_weight[e0 + i] : 1.f;
-    qp[i] = norm_q && mine ? a.q_weight[po + i] : 1.f;
-    kw[i] = norm_k && mine ? a.k_weight[e0 + i] : 1.f;
-    kp[i] = norm_k && mine ? a.k_weight[po + i] : 1.f;
+  if (norm_q) {
+    load_floats<8>(a.q_weight + (mine ? e0 : 0), qw);
+    load_floats<8>(a.q_weight + (mine ? po : 0), qp);
+  }
+  if (norm_k) {
+    load_floats<8>(a.k_weight + (mine ? e0 : 0), kw);
+    load_floats<8>(a.k_weight + (mine ? po : 0), kp);
   }
 
   const int qs = (a.heads + kHeads - 1) / kHeads, ks = (a.kv_heads + kHeads - 1) / kHeads;
@@ -347,21 +364,16 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
     const bool stored = live && page >= 0 && page < a.pages;
     const int64_t at =
         stored ? page * a.page_stride + (int64_t)(slot - page * a.page_size) * a.token_stride : 0;
-    if (live && r.turned) {
+    if (live && a.rot) {
       const float* cs = a.cos_sin + (int64_t)pos * a.rot;
       if (a.interleaved) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          r.cs[i] = cs[e0 / 2 + i];
-          r.sn[i] = cs[half + e0 / 2 + i];
-        }
+        const int p0 = r.turned ? e0 / 2 : 0;
+        load_floats<4>(cs + p0, r.cs);
+        load_floats<4>(cs + half + p0, r.sn);
       } else {
-        const int p0 = r.upper ? e0 - half : e0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          r.cs[i] = cs[p0 + i];
-          r.sn[i] = cs[half + p0 + i];
-        }
+        const int p0 = !r.turned ? 0 : r.upper ? e0 - half : e0;
+        load_floats<8>(cs + p0, r.cs);
+        load_floats<8>(cs + half + p0, r.sn);
       }
     }
     for (int s = s0; s < s1; s += kBatch) {
@@ -399,9 +411,8 @@ template <typename T>
 void launch_rope(const RopeArgs& a, hipStream_t stream) {
   const int64_t items = a.tokens * a.parts, per = kRopeThreads / kWave;
   const int64_t want = (items + per - 1) / per;
-  // four workgroups a compute unit, which stay: a wave loads the norm weights once (16381 tokens of 32 + 16
-  // heads of 128: 93 us, 4.4 TB/s, with 1024 workgroups; 98 with 2048, 110 with one wave a token, 116
-  // with 512)
+  // four workgroups a compute unit, which stay (16381 tokens of 32 + 2 x 8 heads of 128: 86 us; 114 with 512
+  // workgroups, 86 to 88 with 2048 and more)
   const dim3 grid((unsigned)(want < 1024 ? want : 1024));
   if (a.d <= 64)
     hipLaunchKernelGGL((qk_norm_rope_kernel<T, 8>), grid, dim3(kRopeThreads), 0, stream, a);
@@ -491,8 +502,14 @@ extern "C" lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_arg
   a.pages = c.pages; a.page_stride = c.page_stride; a.token_stride = c.token_stride;
   a.head_stride = c.head_stride;
   a.page_size = c.page_size;
-  // few tokens: their heads spread over more waves
-  a.parts = x.tokens >= 4096 ? 1 : x.tokens >= 512 ? 4 : 12;
+  // Few tokens: their steps spread over more waves, one each, or about three each while the waves have
+  // work at once anyway. With 12 steps a token (32 + 2 x 8 heads of 128): 16 tokens 3.6 us as 12 waves, 4.7
+  // as 4, 9.8 as 1; 256 tokens 5.5, 5.1, 10.3; 1024 tokens 12.9, 9.1, 11.8; 2048 tokens 13.3 as 4, 13.0 as
+  // 2, 14.6 as 1; 4096 tokens 22.0, 20.5, 20.1.
+  const int each = c.d <= 64 ? 8 : c.d <= 128 ? 4 : 2;  // heads of a step
+  const int64_t steps = (x.heads + each - 1) / each + 2 * ((c.heads + each - 1) / each);
+  const int64_t fit = 6144 / x.tokens, third = (steps + 2) / 3;
+  a.parts = (int)(x.tokens * steps <= 2400 ? steps : fit < 1 ? 1 : fit < third ? fit : third);
   if (c.dtype == LILICORR_BF16) launch_rope<Bf16>(a, stream);
   else launch_rope<F16>(a, stream);
   return launch_status();
