@@ -181,6 +181,12 @@ ROPE_CASES = [
     (10, 4, 2, 128, 0, torch.float16, False, True, 16, "phd"),
     (600, 4, 1, 64, 64, torch.bfloat16, False, True, 16, "phd"),
     (4100, 2, 1, 32, 32, torch.bfloat16, False, True, 64, "phd"),
+    # a token's heads spread over waves: each step, a third of them, two, none
+    (150, 32, 8, 128, 128, torch.bfloat16, False, True, 16, "kv"),
+    (301, 32, 8, 128, 64, torch.float16, True, True, 16, "phd"),
+    (303, 5, 3, 200, 80, torch.bfloat16, False, True, 16, "phd"),
+    (2101, 8, 2, 128, 128, torch.bfloat16, False, True, 16, "hpd"),
+    (6150, 3, 1, 96, 96, torch.float16, False, True, 32, "phd"),
 ]
 
 
