@@ -20,10 +20,11 @@
 // meet no bank conflicts. Where WR is 1 each wave copies just what it uses and meets no barrier.
 //
 // Softmax: running maximum and sum in fp32. The accumulated output is rescaled only when a
-// row's maximum has grown by more than 2^8 over the one that its powers are taken against (they
+// row's maximum has grown by more than 2^8 over the power of two that its powers are taken against (they
 // are then at most 2^8; fp32 sums and bf16 hold that, and fp16 holds them times 2^7, which it is given).
-// Probabilities are rounded to the cache's type for the matrix cores, and the sum (fp32) is of the rounded
-// ones, as the output is.
+// Probabilities are rounded to the cache's type, once, because the matrix cores multiply 16-bit operands (two
+// terms of a probability would double the second product); the sum (fp32) is of the rounded ones, as the
+// output is, so that weights add up to one. A rescaling is by a power of two and rounds none of them again.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -421,7 +422,8 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
   for (int i = 0; i < C::ND; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m = -__builtin_inff(), l = 0.f;  // the maximum in score units; this half's share of the sum
+  // the power of two that the powers are taken against; this half's share of the sum
+  float m = -__builtin_inff(), l = 0.f;
 
   // LDS offsets of this lane's reads, without the stage
   const uint32_t sub = (uint32_t)wk * (C::KB * 32);  // first key of the wave's share of a stage
@@ -539,7 +541,8 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
         }
       }
     };
-    // masks the block's scores and brings the maximum up to it
+    // masks the block's scores and brings the maximum up to it: to a whole power of two, so that what is
+    // there already changes by an exact factor
     auto maximum = [&](int b) {
       if (!whole) {
 #pragma unroll
@@ -550,11 +553,12 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
 #pragma unroll
       for (int e = 1; e < 15; e += 2) mx = max3(mx, sc[b][e], sc[b][e + 1]);
       mx = cross_max(max3(mx, sc[b][15], mx));
-      const bool grows = (mx - m) * a.scale2 > kRescale;  // -inf - -inf is NaN and does not count
+      const bool grows = fmaf(mx, a.scale2, -m) > kRescale;  // -inf - -inf is NaN and does not count
       if (__ballot(grows)) {
-        // nothing is accumulated while m is -inf; rows that need not change keep their values exactly
-        const float f = !grows ? 1.f : m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mx) * a.scale2);
-        m = grows ? mx : m;
+        // nothing is accumulated while m is -inf
+        const float up = __builtin_floorf(mx * a.scale2);
+        const float f = grows ? __builtin_amdgcn_ldexpf(1.f, (int)fmaxf(m - up, -300.f)) : 1.f;
+        m = grows ? up : m;
         l *= f;
 #pragma unroll
         for (int i = 0; i < C::ND; ++i)
@@ -586,7 +590,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
         load_v(2);
       }
       maximum(b);
-      ms = m == -__builtin_inff() ? 0.f : m * a.scale2 - kLift<T>;
+      ms = m == -__builtin_inff() ? 0.f : m - kLift<T>;
       if (b + 1 < C::KB) {
 #pragma unroll
         for (int i = 0; i < kQK; ++i) {
@@ -647,7 +651,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
 
   // ---- join the waves that shared the keys ---------------------------------------------------------
   l = cross_sum(l);
-  float mp = m * a.scale2 - kLift<T>;  // in powers of two
+  float mp = m - kLift<T>;
   if constexpr (C::WK > 1) {
     constexpr uint32_t kMl = C::kWaves * 32 * C::D * 4;
 #pragma unroll
