@@ -500,11 +500,13 @@ lilicorr_status lilicorr_scorer_forward(float *X, int64_t N, int64_t S, int K, i
  * again by the next call. An ended request gives back every page it holds: its row's first
  * min(ceil(S/P), end) entries and then entries since .. end - 1.
  *   pages_out  [N][2] int32, cursor_out [3] int64 (the third: pages that were lacking): for the next
- *              call. They must not overlap the inputs: workgroups read those while others write.
+ *              call.
  *   starts     [N + 1] int32: tokens of the requests before n (prefix sums of max(incoming, 0),
  *              at most `tokens`); totals [N] int32: lengths + incoming (0 for an ended request).
  *   slots      [tokens] int32: page * P + position % P of each new token, request by request, -1
  *              where it has no page; positions [tokens] int32. Past starts[N] both are -1.
+ * No output (table and queue among them) may overlap another one or an input, totals not even lengths:
+ * workgroups read those while others write (LILICORR_ERR_INVALID_ARG).
  * Drafts that were rejected need nothing: call with the shorter length, the pages stay.
  * Limits: 1 <= N <= 4096, 1 <= P <= 65536, P * M < 2^31, 0 <= tokens < 2^31, C < 2^31.
  */

@@ -448,6 +448,17 @@ extern "C" lilicorr_status lilicorr_page_plan(const lilicorr_page_plan_args* arg
       !aligned8(x.cursor_out) || !aligned4(x.starts) || !aligned4(x.totals) || !aligned4(x.slots) ||
       !aligned4(x.positions))
     return LILICORR_ERR_ALIGNMENT;
+  // workgroups read what others' outputs would lie on: only the arrays that are not written may share memory
+  constexpr int kRead = 4;
+  const size_t n4 = (size_t)x.N * 4, t4 = (size_t)x.tokens * 4;
+  const struct { const void* at; size_t bytes; } parts[] = {
+      {x.lengths, n4}, {x.incoming, n4}, {x.pages, 2 * n4}, {x.cursor, 24},
+      {x.table, n4 * (size_t)x.table_width}, {x.queue, (size_t)x.queue_size * 4}, {x.pages_out, 2 * n4},
+      {x.cursor_out, 24}, {x.starts, n4 + 4}, {x.totals, n4}, {x.slots, t4}, {x.positions, t4}};
+  constexpr int kParts = sizeof(parts) / sizeof(parts[0]);
+  for (int i = kRead; i < kParts; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(parts[i].at, parts[i].bytes, parts[j].at, parts[j].bytes)) return LILICORR_ERR_INVALID_ARG;
   PlanArgs a;
   a.lengths = x.lengths; a.incoming = x.incoming; a.pages = x.pages;
   a.table = x.table; a.queue = x.queue; a.cursor = x.cursor;
