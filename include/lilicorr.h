@@ -497,12 +497,17 @@ lilicorr_status lilicorr_scorer_forward(float *X, int64_t N, int64_t S, int K, i
  *              first ceil(S / P) go back to the queue. Their table entries keep their value.
  * A request needs ceil((lengths + incoming) / P) entries, M at most; the ones it lacks are taken from
  * the queue's head, requests in order. Where the queue runs out, an entry gets -1 and is asked for
- * again by the next call. An ended request gives back every page it holds: its row's first
+ * again by the next call. Tokens without a page are stored nowhere, and the request goes on without them:
+ * lengths[n] counts as at most pages[n][0] P, so that the next call's tokens take their positions, and what
+ * earlier owners left on the pages that come later is never read as keys. min(totals[n], pages_out[n][0] P)
+ * tokens are stored after the step; a server that wants the rest gives them again, and cursor_out[2] says
+ * whether there are any. An ended request gives back every page it holds: its row's first
  * min(ceil(S/P), end) entries and then entries since .. end - 1.
  *   pages_out  [N][2] int32, cursor_out [3] int64 (the third: pages that were lacking): for the next
  *              call.
  *   starts     [N + 1] int32: tokens of the requests before n (prefix sums of max(incoming, 0),
- *              at most `tokens`); totals [N] int32: lengths + incoming (0 for an ended request).
+ *              at most `tokens`); totals [N] int32: lengths + incoming (0 for an ended request), the
+ *              tokens without a page among them: the attentions see no key on a page that is not there.
  *   slots      [tokens] int32: page * P + position % P of each new token, request by request, -1
  *              where it has no page; positions [tokens] int32. Past starts[N] both are -1.
  * No output (table and queue among them) may overlap another one or an input, totals not even lengths:

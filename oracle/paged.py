@@ -8,7 +8,8 @@ import numpy as np
 
 def page_plan(lengths, incoming, pages, table, queue, cursor, page_size, tokens, window=0, sinks=0):
     """One request after the other, one page after the other. table and queue are not changed; the
-    new ones come back with the other outputs."""
+    new ones come back with the other outputs. Tokens for which there was no page are not part of their
+    request: it holds at most as many as its pages do."""
     P, M, C = page_size, table.shape[1], len(queue)
     table, queue = table.copy(), queue.copy()
     head, tail = int(cursor[0]), int(cursor[1])
@@ -24,6 +25,7 @@ def page_plan(lengths, incoming, pages, table, queue, cursor, page_size, tokens,
             totals.append(0)
             starts.append(starts[-1])
             continue
+        L = min(L, end * P)
         # entries whose every token is behind the first query's window
         gone = []
         if window:

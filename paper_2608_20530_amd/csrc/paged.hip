@@ -36,6 +36,15 @@ struct PlanArgs {
   int32_t *starts, *totals, *slots, *positions;
 };
 
+// entries of a request's table row that are filled
+__device__ __forceinline__ int row_end(const PlanArgs& a, int n) { return min(max(a.pages[2 * n], 0), a.M); }
+
+// The tokens that a request holds: those that there were no pages for were never stored, and the pages
+// that it gets now hold something else where they would be.
+__device__ __forceinline__ int row_length(const PlanArgs& a, int n, int end) {
+  return min(max(a.lengths[n], 0), end * a.P);  // P * M < 2^31
+}
+
 struct PlanRow {
   int64_t total;
   int fresh, take, give, end, since, kept;
@@ -44,8 +53,9 @@ struct PlanRow {
 
 __device__ __forceinline__ PlanRow plan_row(const PlanArgs& a, int n) {
   PlanRow r;
-  const int L = max(a.lengths[n], 0), I = a.incoming[n];
-  r.end = min(max(a.pages[2 * n], 0), a.M);
+  const int I = a.incoming[n];
+  r.end = row_end(a, n);
+  const int L = row_length(a, n, r.end);
   r.since = max(max(a.pages[2 * n + 1], 0), a.first);
   r.kept = min(a.first, r.end);
   r.ended = I < 0;
@@ -164,9 +174,9 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a) {
       int slot = -1, pos = -1;
       if (i < fresh) {
         const int n = find_row(s_tok, a.N, (int)i);
-        pos = clamp32((int64_t)max(a.lengths[n], 0) + ((int)i - s_tok[n]));
+        const int end = row_end(a, n);
+        pos = clamp32((int64_t)row_length(a, n, end) + ((int)i - s_tok[n]));
         const int e = pos / a.P;
-        const int end = min(max(a.pages[2 * n], 0), a.M);
         int page = -1;
         if (e < end) {
           page = a.table[(int64_t)n * a.M + e];
@@ -181,7 +191,7 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a) {
     } else if (i < a.tokens + take) {  // a taken page into its table row
       const int g = (int)(i - a.tokens);
       const int n = find_row(s_take, a.N, g);
-      const int e = min(max(a.pages[2 * n], 0), a.M) + (g - s_take[n]);
+      const int e = row_end(a, n) + (g - s_take[n]);
       if (e < a.M) a.table[(int64_t)n * a.M + e] = g < avail ? a.queue[ring(at_head, g)] : -1;
     } else {  // a page that goes back to the queue
       const int g = (int)(i - a.tokens - take);

@@ -150,7 +150,8 @@ def page_plan(lengths: torch.Tensor, incoming: torch.Tensor, pages: torch.Tensor
               tokens: int, window: int = 0, sinks: int = 0, out: PagePlan | None = None) -> PagePlan:
     """One step's places. lengths, incoming [N], pages [N, 2] int32; table [N, M] and queue [C] int32
     are updated in place; cursor [3] int64. `tokens` rows of slots and positions are made (at least
-    the new tokens of the step). `out` must not share memory with the other arguments."""
+    the new tokens of the step). Where cursor[2] of the result is not 0 the queue ran out: request n has
+    stored min(totals[n], pages[n, 0] * page_size) tokens, and the next step goes on from there. `out` must not share memory with the other arguments."""
     (N,), M, (C,) = lengths.shape, table.shape[-1], queue.shape
     n = (N,)
     if out is None:
