@@ -508,6 +508,8 @@ lilicorr_status lilicorr_scorer_forward(float *X, int64_t N, int64_t S, int K, i
  *   starts     [N + 1] int32: tokens of the requests before n (prefix sums of max(incoming, 0),
  *              at most `tokens`); totals [N] int32: lengths + incoming (0 for an ended request), the
  *              tokens without a page among them: the attentions see no key on a page that is not there.
+ *              New tokens past the first `tokens` of a step are not taken: starts and totals leave them
+ *              out (their pages, if any, stay with the request, as those of rejected drafts do).
  *   slots      [tokens] int32: page * P + position % P of each new token, request by request, -1
  *              where it has no page; positions [tokens] int32. Past starts[N] both are -1.
  * No output (table and queue among them) may overlap another one or an input, totals not even lengths:

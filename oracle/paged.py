@@ -9,7 +9,7 @@ import numpy as np
 def page_plan(lengths, incoming, pages, table, queue, cursor, page_size, tokens, window=0, sinks=0):
     """One request after the other, one page after the other. table and queue are not changed; the
     new ones come back with the other outputs. Tokens for which there was no page are not part of their
-    request: it holds at most as many as its pages do."""
+    request: it holds at most as many as its pages do. Nor are the ones past the `tokens`-th row."""
     P, M, C = page_size, table.shape[1], len(queue)
     table, queue = table.copy(), queue.copy()
     head, tail = int(cursor[0]), int(cursor[1])
@@ -40,14 +40,15 @@ def page_plan(lengths, incoming, pages, table, queue, cursor, page_size, tokens,
             else:
                 table[n, e] = -1
                 lacking += 1
-        for p in range(L, L + new):
+        rows = min(new, tokens - starts[-1])
+        for p in range(L, L + rows):
             e = p // P
             page = int(table[n, e]) if e < held else -1
             slots.append(page * P + p % P if page >= 0 else -1)
             positions.append(p)
         pages_out.append((held, since + len(gone)))
-        totals.append(L + new)
-        starts.append(starts[-1] + new)
+        totals.append(L + rows)
+        starts.append(starts[-1] + rows)
     for i, page in enumerate(back):
         queue[(tail + i) % C] = page
     pad = [-1] * (tokens - len(slots))

@@ -155,7 +155,9 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a) {
       const int granted = max(min(r.take, avail - min(s_take[n], avail)), 0);
       a.pages_out[2 * n] = r.ended ? 0 : r.end + granted;
       a.pages_out[2 * n + 1] = r.ended ? 0 : r.since + r.give;
-      a.totals[n] = clamp32(r.total);
+      // a token past the last row is not taken: it counts neither here nor in starts
+      const int64_t rows = a.tokens > s_tok[n] ? a.tokens - s_tok[n] : 0;
+      a.totals[n] = clamp32(r.total - (r.fresh > rows ? r.fresh - rows : 0));
     }
     for (int n = tid; n <= a.N; n += kPlanThreads)
       a.starts[n] = s_tok[n] < a.tokens ? s_tok[n] : (int)a.tokens;
