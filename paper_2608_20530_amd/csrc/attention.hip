@@ -12,6 +12,9 @@ namespace lilicorr {
 namespace {
 
 constexpr size_t kLeastBytes = 256;  // of a workspace
+// The longest sequences have so many tokens: lengths, windows and sinks past it say "without end"
+constexpr int64_t kMost = (int64_t)1 << 30;
+int64_t bounded(int64_t n) { return n < kMost ? n : kMost; }
 
 // One pass over keys: which tile height, how many tiles and chunks
 struct Pass {
@@ -108,7 +111,6 @@ lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p
   if (a.sinks > 0 && a.window == 0) return LILICORR_ERR_INVALID_ARG;
   if (shared ? (a.shared_length < 1 || a.window != 0) : a.shared_length != 0)
     return LILICORR_ERR_INVALID_ARG;
-  constexpr int64_t kMost = (int64_t)1 << 30;
   if (a.heads > 65535 || a.N > (1 << 20) || a.tokens > kMost / a.heads ||
       a.table_width > kMost / a.cache.page_size || a.shared_length > kMost)
     return LILICORR_ERR_UNSUPPORTED;
@@ -132,7 +134,7 @@ lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p
     // a tile's queries see at most this many: from the first one's window to the last one itself, or
     // to the request's last token
     const int64_t tile_tokens = BM / group + 1;
-    const int64_t seen = a.window + a.sinks +
+    const int64_t seen = bounded(a.window) + bounded(a.sinks) +
                          (a.causal && tile_tokens < max_tokens ? tile_tokens : max_tokens);
     if (seen < keys) keys = seen;
   }
@@ -247,14 +249,13 @@ lilicorr_status run(const lilicorr_attention_args& x, const Plan& p, hipStream_t
   a.token_units = (uint32_t)(c.token_stride / unit);
   a.unit_bytes = (uint32_t)(unit * 2);
   a.scale2 = x.scale * 1.4426950408889634f;
-  constexpr int64_t kMost = 1 << 30;
   a.own = attn_pass(p.tail, c.heads, p.shared ? p.first.chunks : 0);
   a.own.table = x.table;
   a.own.table_width = (int)x.table_width;
   a.own.max_tokens = (int)(x.max_tokens < x.tokens ? x.max_tokens : x.tokens);
-  a.own.max_length = (int)(x.max_length < kMost ? x.max_length : kMost);
-  a.own.window = (int)(x.window < kMost ? x.window : kMost);
-  a.own.sinks = (int)(x.sinks < kMost ? x.sinks : kMost);
+  a.own.max_length = (int)bounded(x.max_length);
+  a.own.window = (int)bounded(x.window);
+  a.own.sinks = (int)bounded(x.sinks);
   a.own.causal = x.causal != 0;
   if (p.shared) {
     a.shared = attn_pass(p.first, c.heads, 0);
