@@ -558,7 +558,8 @@ typedef struct {
  *   v_stride elements from token to token (multiples of 8: views of one projection's output fit).
  *   q_weight, k_weight [d] fp32 or NULL; cos_sin [max_positions][rot] fp32, rot / 2 cosines and then
  *   rot / 2 sines a row.
- *   q_out [tokens][heads][d], contiguous; it may be q itself.
+ *   q_out [tokens][heads][d], contiguous; it may be q itself, and must not overlap q's, k's or v's rows
+ *   otherwise (LILICORR_ERR_INVALID_ARG).
  * Two tokens of a call must not have the same slot. Limits: rot a multiple of 16, 0 <= rot <= d
  * (cos_sin may be NULL when 0); tokens < 2^31.
  */
@@ -597,7 +598,7 @@ lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_args *args, hi
  * Limits: heads a multiple of cache heads, at most 65535; tokens * heads, page_size * table_width and
  * shared_length at most 2^30; N at most 2^20; every element of the cache less than
  * 2^32 * gcd(page_stride, token_stride) elements from its start; scale > 0 and finite. out must not
- * overlap q.
+ * overlap q's rows (LILICORR_ERR_INVALID_ARG).
  */
 typedef struct {
     const void *q;                  /* [tokens][heads][d] of the cache's dtype */

@@ -296,6 +296,9 @@ lilicorr_status attention(const lilicorr_attention_args* a, bool shared, hipStre
     return LILICORR_ERR_ALIGNMENT;
   if (!a->workspace || a->workspace_bytes < p.bytes) return LILICORR_ERR_WORKSPACE;
   if (a->max_tokens == 0) return LILICORR_OK;
+  const size_t row = (size_t)a->heads * a->cache.d * 2;
+  if (rows_overlap(a->q, a->q_stride * 2, row, a->tokens, a->out, row * (size_t)a->tokens))
+    return LILICORR_ERR_INVALID_ARG;
   return a->cache.dtype == LILICORR_BF16 ? run<Bf16>(*a, p, stream) : run<F16>(*a, p, stream);
 }
 

@@ -512,6 +512,12 @@ extern "C" lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_arg
       !aligned16(c.k) || !aligned16(c.v) || !aligned16(x.cos_sin) || !aligned16(x.q_weight) ||
       !aligned16(x.k_weight) || !aligned4(x.slots) || !aligned4(x.positions))
     return LILICORR_ERR_ALIGNMENT;
+  // what other waves still read must not lie where q_out does
+  const size_t q_row = (size_t)x.heads * c.d * 2, k_row = (size_t)c.heads * c.d * 2, out_bytes = q_row * (size_t)x.tokens;
+  if ((x.q_out != x.q && rows_overlap(x.q, x.q_stride * 2, q_row, x.tokens, x.q_out, out_bytes)) ||
+      rows_overlap(x.k, x.k_stride * 2, k_row, x.tokens, x.q_out, out_bytes) ||
+      rows_overlap(x.v, x.v_stride * 2, k_row, x.tokens, x.q_out, out_bytes))
+    return LILICORR_ERR_INVALID_ARG;
   RopeArgs a;
   a.q = (const uint16_t*)x.q; a.k = (const uint16_t*)x.k; a.v = (const uint16_t*)x.v;
   a.q_stride = x.q_stride; a.k_stride = x.k_stride; a.v_stride = x.v_stride;

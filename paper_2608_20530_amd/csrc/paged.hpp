@@ -52,6 +52,14 @@ inline bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y ? a_bytes > y - x && b_bytes > 0 : b_bytes > x - y && a_bytes > 0;
 }
+// whether one of `rows` rows, `stride` bytes apart, has a byte in common with a stretch of memory
+inline bool rows_overlap(const void* a, int64_t stride, size_t row_bytes, int64_t rows, const void* b,
+                         size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  // the first row that ends past the stretch's beginning
+  const uint64_t first = x + row_bytes > y ? 0 : stride ? (y - x - row_bytes) / (uint64_t)stride + 1 : (uint64_t)rows;
+  return first < (uint64_t)rows && x + first * (uint64_t)stride < y + b_bytes;
+}
 inline bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s < ((int64_t)1 << 40); }
 
 // sizes of a cache, without its pointers
