@@ -37,15 +37,47 @@ struct Plan {
 // tiles of eight waves 650 us against 629 with 128 for a prefill of 8192 tokens.
 int tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
-// Keys of a kernel's stage, and its workgroups that run at once on 256 compute units (LDS and, for 128
-// rows, registers)
+// Calls `use` with the kernel of a width and tile height: waves of rows x waves of keys, 32-key blocks a wave and
+// stage, stages of the ring. Few rows: four waves share the keys and each keeps its own ring; more: barriers,
+// 64 keys a stage, and a ring of two so that two workgroups share a compute unit (a ring of four with one: 302
+// against 188 us for 64 blocks of 16 tokens behind 4096 keys).
+template <typename T, bool FULL, int D, typename F>
+auto with_rows(int BM, const F& use) {
+  if constexpr (D <= 64) {
+    if (BM == 32) return use(AttnConfig<T, FULL, D, 1, 4, 1, 4>());
+    if (BM == 64) return use(AttnConfig<T, FULL, D, 2, 2, 1, 4>());
+    return use(AttnConfig<T, FULL, D, 4, 1, 2, 2>());
+  } else if constexpr (D <= 128) {
+    if (BM == 32) return use(AttnConfig<T, FULL, D, 1, 4, 1, 2>());
+    if (BM == 64) return use(AttnConfig<T, FULL, D, 2, 2, 1, 2>());
+    return use(AttnConfig<T, FULL, D, 4, 1, 2, 2>());
+  } else {
+    if (BM == 32) return use(AttnConfig<T, FULL, D, 1, 2, 1, 2>());
+    if (BM == 64) return use(AttnConfig<T, FULL, D, 2, 2, 1, 2>());
+    return use(AttnConfig<T, FULL, D, 4, 1, 1, 2>());
+  }
+}
+
+// Heads between the powers of two lie in LDS rows of the next one, and elements past their width are copied from
+// zeros. Heads of 65 to 96 leave out the empty quarter of the products (a ragged prefill with heads of 80: 175 us
+// against 196).
+template <typename T, typename F>
+auto with_kernel(int d, int BM, const F& use) {
+  if (d == 64) return with_rows<T, true, 64>(BM, use);
+  if (d < 64) return with_rows<T, false, 64>(BM, use);
+  if (d <= 96) return with_rows<T, false, 96>(BM, use);
+  if (d == 128) return with_rows<T, true, 128>(BM, use);
+  if (d < 128) return with_rows<T, false, 128>(BM, use);
+  if (d == 256) return with_rows<T, true, 256>(BM, use);
+  return with_rows<T, false, 256>(BM, use);
+}
+
+// Keys of a kernel's stage, and its workgroups that run at once on 256 compute units
 struct Fit {
   int stage, slots;
 };
 Fit kernel_fit(int d, int BM) {
-  const int stage = d <= 128 ? (BM == 32 ? 128 : 64) : (BM == 128 ? 32 : 64);
-  const int each = d <= 64 ? (BM == 32 ? 1 : BM == 64 ? 2 : 3) : d <= 128 ? (BM == 32 ? 1 : 2) : 1;
-  return {stage, 256 * each};
+  return with_kernel<Bf16>(d, BM, [](auto c) { return Fit{decltype(c)::SK, 256 * decltype(c)::kAtOnce}; });
 }
 
 // A pass's row tiles (of all heads) and the stages of keys that a tile sees at most
@@ -173,41 +205,6 @@ void launch(const AttnArgs& a, hipStream_t stream) {
                      dim3(C::kThreads), C::kLds, stream, a);
 }
 
-// The kernels of a width: waves of rows x waves of keys, 32-key blocks a wave and stage, stages of the
-// ring. Few rows: four waves share the keys and each keeps its own ring; more: barriers, 64 keys a
-// stage, and a ring of two so that two workgroups share a compute unit (a ring of four with one: 302
-// against 188 us for 64 blocks of 16 tokens behind 4096 keys).
-template <typename T, bool FULL, int D>
-void launch_rows(const AttnArgs& a, int BM, hipStream_t stream) {
-  if constexpr (D <= 64) {
-    if (BM == 32) launch<AttnConfig<T, FULL, D, 1, 4, 1, 4>>(a, stream);
-    else if (BM == 64) launch<AttnConfig<T, FULL, D, 2, 2, 1, 4>>(a, stream);
-    else launch<AttnConfig<T, FULL, D, 4, 1, 2, 2>>(a, stream);
-  } else if constexpr (D <= 128) {
-    if (BM == 32) launch<AttnConfig<T, FULL, D, 1, 4, 1, 2>>(a, stream);
-    else if (BM == 64) launch<AttnConfig<T, FULL, D, 2, 2, 1, 2>>(a, stream);
-    else launch<AttnConfig<T, FULL, D, 4, 1, 2, 2>>(a, stream);
-  } else {
-    if (BM == 32) launch<AttnConfig<T, FULL, D, 1, 2, 1, 2>>(a, stream);
-    else if (BM == 64) launch<AttnConfig<T, FULL, D, 2, 2, 1, 2>>(a, stream);
-    else launch<AttnConfig<T, FULL, D, 4, 1, 1, 2>>(a, stream);
-  }
-}
-
-// Heads between the powers of two lie in LDS rows of the next one, and elements past their width are copied from
-// zeros. Heads of 65 to 96 leave out the empty quarter of the products (a ragged prefill with heads of 80: 175 us
-// against 196).
-template <typename T>
-void launch_attention(const AttnArgs& a, int BM, hipStream_t stream) {
-  if (a.d == 64) launch_rows<T, true, 64>(a, BM, stream);
-  else if (a.d < 64) launch_rows<T, false, 64>(a, BM, stream);
-  else if (a.d <= 96) launch_rows<T, false, 96>(a, BM, stream);
-  else if (a.d == 128) launch_rows<T, true, 128>(a, BM, stream);
-  else if (a.d < 128) launch_rows<T, false, 128>(a, BM, stream);
-  else if (a.d == 256) launch_rows<T, true, 256>(a, BM, stream);
-  else launch_rows<T, false, 256>(a, BM, stream);
-}
-
 AttnPass attn_pass(const Pass& p, int kv_heads, int slot0) {
   AttnPass r = {};
   r.tiles = p.tiles;
@@ -268,7 +265,7 @@ lilicorr_status run(const lilicorr_attention_args& x, const Plan& p, hipStream_t
   a.split = p.slots > 1;
   a.part_o = (float*)w;
   a.part_ml = (f32x2_t*)(w + (size_t)p.slots * p.rows * c.d * 4);
-  launch_attention<T>(a, p.BM, stream);
+  with_kernel<T>(a.d, p.BM, [&](auto c) { launch<decltype(c)>(a, stream); });
   if (a.split) {
     if (c.d <= 64) launch_join<T, 16>(a, p, stream);
     else if (c.d <= 128) launch_join<T, 32>(a, p, stream);

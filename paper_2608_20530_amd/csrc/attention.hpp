@@ -174,6 +174,12 @@ struct AttnConfig {
   static constexpr int kEntries = 256;
   static constexpr uint32_t kFlag = kPages + kWaves * kEntries * 4;
   static constexpr size_t kLds = kFlag + 16;
+  // waves of a SIMD, which the kernel's registers are given out for, and workgroups that a compute unit
+  // holds with them and its 160 KB of LDS
+  static constexpr int kSimdWaves = DP > 128 ? 1 : 2;
+  static constexpr int kByWaves = 4 * kSimdWaves / kWaves, kByLds = 160 * 1024 / (int)kLds;
+  static constexpr int kAtOnce = kByWaves < kByLds ? kByWaves : kByLds;
+  static_assert(kAtOnce >= 1, "a workgroup fits");
   static_assert(KB <= 2, "blocks of a stage and wave");
   static_assert(WROWS % RPI == 0 && WROWS <= kWave, "whole copy instructions");
 };
@@ -746,7 +752,7 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
 // 256 registers; tiles of 256 rows in eight waves take 650 us, deeper operand rings and wave priorities
 // gain nothing.
 template <typename C>
-__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::DP > 128 ? 1 : 2, C::DP > 128 ? 1 : 2)))
+__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kSimdWaves, C::kSimdWaves)))
 void attention_kernel(AttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char attn_smem[];
   const int item = (int)blockIdx.x - a.shared.items;
