@@ -131,7 +131,7 @@ def serve(steps=6, N=8, B=16, K=8, V=32000, hidden=256, prompt=200, window=128, 
         accepted = torch.randint(1, B + 1, (N,), generator=g, device="cuda", dtype=torch.int32)
         # from the step's totals: a request whose pages ran out is shorter than its last one's says
         layer.keep(layer.lengths - (B - accepted))
-        if s % 3 == 2:  # a request ends, and a new one of one token takes its place
+        if s % 3 == 2:  # a request ends; the next block begins a new one in its place
             ends = torch.where(torch.arange(N, device="cuda") == s % N, -1, 0).to(torch.int32)
             layer.step(torch.empty(0, hidden, dtype=dt, device="cuda"), ends, 0, 0)
     return torch.stack(drafts), layer

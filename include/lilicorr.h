@@ -553,7 +553,7 @@ typedef struct {
  * q_out, k and (as it is) v to the cache at slots[t]; a token with slots[t] outside the cache
  * (-1: no page) is not written there. A position below 0 (the rows past the last token of
  * lilicorr_page_plan) or, with a rotation, of max_positions or more gives zeros in q_out and no cache
- * write.
+ * write: sequences must end before max_positions, or the attentions see what was at such a token's place.
  *   q [tokens][heads][d], k, v [tokens][cache heads][d] of the cache's dtype; q_stride, k_stride,
  *   v_stride elements from token to token (multiples of 8: views of one projection's output fit).
  *   q_weight, k_weight [d] fp32 or NULL; cos_sin [max_positions][rot] fp32, rot / 2 cosines and then
@@ -591,7 +591,8 @@ lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_args *args, hi
  * product, and the output once more. The result does not depend on what else runs, and is the same
  * on every call with the same arguments.
  *   max_tokens, max_length   upper bounds of T and totals that the host knows (they choose tiles and
- *       how far the key axis is split). Keys past them are not seen; the output of queries past them,
+ *       how far the key axis is split). Keys past them are not seen; the output of queries past them
+ *       (of all queries of a request with more than max_tokens, where there is a window and not `causal`),
  *       and of rows past starts[N], has no meaning (zeros, what it held, or anything else).
  *   workspace   device scratch of the size the query gives, caller-owned; what it holds before or after
  *       a call does not matter. Calls sharing it must not overlap.

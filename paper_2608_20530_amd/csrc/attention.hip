@@ -34,7 +34,7 @@ struct Plan {
 // The least height that holds a request's rows: fewer rows than a tile has are computed all the same. Single tokens
 // in 32-row tiles share the keys among the four waves (two waves a tile: 822 us and more against 762 for 256 tokens);
 // the 64 rows of a block of 16 with four query heads a key head as 2 x 2 waves take 196 us, as 2 x 4 202; 256-row
-// tiles of eight waves 650 us against 629 with 128 for a prefill of 8192 tokens.
+// tiles of eight waves 650 us against 629 with 128 for a prefill of 8192 tokens (both on an earlier version).
 int tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
 // Calls `use` with the kernel of a width and tile height: waves of rows x waves of keys, 32-key blocks a wave and
@@ -89,7 +89,10 @@ struct Work {
 // begins and ends for about three (page numbers, queries, first copies; output). As long as all run at
 // once the longest one counts, else also the work of all over the workgroups that run at once, and half
 // of a last one. Split keys add the join's launch (two and a half) and fp32 partial outputs that are written
-// and read again, at 5 TB/s against 1.5 us a stage.
+// and read again, at 5 TB/s against 1.5 us a stage. The times in stages were fitted to heads of 128, where the
+// chosen length is the best one for one token (13.5 us) and 32 tokens behind a prefix (30.4), and within 3% for 64
+// blocks behind one (357 against 347). Narrower heads have shorter stages: 4% for a ragged batch with heads of 64
+// (23.1 against 22.1) and 10% for a prefix with heads of 80 (21.2 against 19.2).
 int64_t chunk_stages(const Work& shared, const Work& own, int slots, int64_t out_elements) {
   const int64_t longest = shared.stages > own.stages ? shared.stages : own.stages;
   int64_t best = longest, last = 0;
@@ -179,7 +182,8 @@ lilicorr_status make_plan(const lilicorr_attention_args& a, bool shared, Plan& p
   p.BM = BM;
   // where every key is read once, runs of items keep a request's heads on one XCD (their tokens lie side
   // by side, and eight XCDs with a head each would use an eighth of every L2: 825 against 1068 us for 256
-  // tokens); tiles that share keys find them in the L2 of their head's XCD (prefill 664 against 772 us)
+  // tokens); tiles that share keys find them in the L2 of their head's XCD (prefill 664 against 772 us;
+  // these figures too are of an earlier version)
   p.tail = make_pass(tiles, own_work.stages, chunk, fit.stage, own <= BM);
   p.slots = p.tail.chunks;
   if (shared) {

@@ -17,7 +17,8 @@
 // position i is key i below the number of sinks and key i + shift above. Stages of 32 KB WK keys
 // of that list go to LDS by DMA, 16 bytes a lane from wherever the page table says, into a ring of
 // NS stages. Sixteen-byte pieces are permuted within each row as they are copied so that the reads
-// meet no bank conflicts. Where WR is 1 each wave copies just what it uses and meets no barrier.
+// meet no bank conflicts (counted: none with heads of 128; with heads of 64 about one cycle a read is left).
+// Where WR is 1 each wave copies just what it uses and meets no barrier.
 //
 // Softmax: running maximum and sum in fp32. The accumulated output is rescaled only when a
 // row's maximum has grown by more than 2^8 over the power of two that its powers are taken against (they
@@ -205,7 +206,9 @@ struct Keys {
 };
 
 // One row by one wave, key by key, in fp32: what a tile falls back to when a value among the keys that
-// not all of its rows see is infinite or NaN. A lane has four elements of the head.
+// not all of its rows see is infinite or NaN. A lane has four elements of the head. A last resort, half a
+// microsecond a row and key: one infinite value at the edge of one request's mask makes a call of 64 blocks of 16
+// behind 4000 keys take 36 ms instead of 0.2.
 template <typename T>
 __device__ __forceinline__ void attention_row(const AttnArgs& a, const AttnPass& ps, const Keys keys,
                                              int start, int pos0, int head, int r, int64_t part_row,
@@ -745,10 +748,11 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, const AttnPass
 // workgroups are there to read it; 765 us for 256 requests of one token and 100 to 8100 keys (5.65 TB/s),
 // 195 us for 64 blocks of 16 behind windows of 4096 (5.2 TB/s). One request: a chain of dependent loads
 // (lengths, page numbers, first keys: 2.9, 1.4 and 2 to 5 us cold), 10 us for one token behind a window of
-// 4096. Many rows: instruction issue; 575 to 615 us (895 to 957 TFLOP/s) for 8192 tokens behind windows of
-// 4096, where matrix instructions run 43% of the time and about 230 vector instructions for 64 keys and 32
-// rows want the same issue slots. What 64 keys of a wave cost there, found by leaving a part out: powers 65 us,
-// copies 87, edges of masks 26, the test of the maximum 17, page numbers 10. Two waves a SIMD need at most
+// 4096. Many rows: how far the two waves of a SIMD overlap; 585 to 615 us (895 to 941 TFLOP/s) for 8192 tokens
+// behind windows of 4096. Of the SIMDs' cycles 43% have a matrix instruction running and 38% another vector
+// instruction, 16% both and about a third neither (counted; waves spend 29% of their time at waits and barriers).
+// What 64 keys of a wave cost there, found by leaving a part out: powers 65 us, copies 87, edges of masks 26, the
+// test of the maximum 17, page numbers 10. Two waves a SIMD need at most
 // 256 registers; tiles of 256 rows in eight waves take 650 us, deeper operand rings and wave priorities
 // gain nothing.
 template <typename C>

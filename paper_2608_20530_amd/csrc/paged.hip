@@ -534,7 +534,7 @@ extern "C" lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_arg
   // Few tokens: their steps spread over more waves, one each, or about three each while the waves have
   // work at once anyway. With 12 steps a token (32 + 2 x 8 heads of 128): 16 tokens 3.6 us as 12 waves, 4.7
   // as 4, 9.8 as 1; 256 tokens 5.5, 5.1, 10.3; 1024 tokens 12.9, 9.1, 11.8; 2048 tokens 13.3 as 4, 13.0 as
-  // 2, 14.6 as 1; 4096 tokens 22.0, 20.5, 20.1.
+  // 2, 14.6 as 1; 4096 tokens 22.0, 20.5, 20.1. The two limits were chosen there, for all widths.
   const int each = c.d <= 64 ? 8 : c.d <= 128 ? 4 : 2;  // heads of a step
   const int64_t steps = (x.heads + each - 1) / each + 2 * ((c.heads + each - 1) / each);
   const int64_t fit = 6144 / x.tokens, third = (steps + 2) / 3;
