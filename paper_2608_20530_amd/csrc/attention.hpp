@@ -49,8 +49,8 @@ typedef __attribute__((address_space(3))) unsigned char* lds_t;
 
 constexpr int kWaitLoads = 0x0f70;  // s_waitcnt vmcnt(0) alone
 constexpr float kRescale = 8.f;  // growth of the maximum, in powers of two, that is let pass
-// The power that the maximum's probability gets: fp16 ends at 2^16, and its steps of 2^-24 would lose a long
-// run of small probabilities beside one of 1
+// The power of two that the powers' reference is given (the maximum's lies at most 2^8 above it): fp16 ends at
+// 2^16, and its steps of 2^-24 would lose a long run of small probabilities beside one of 1
 template <typename T>
 constexpr float kLift = 0.f;
 template <>
