@@ -625,6 +625,151 @@ size_t lilicorr_prefix_attention_workspace_bytes(const lilicorr_attention_args *
 lilicorr_status lilicorr_window_attention(const lilicorr_attention_args *args, hipStream_t stream);
 lilicorr_status lilicorr_prefix_attention(const lilicorr_attention_args *args, hipStream_t stream);
 
+/*
+ * The cache in 4 bits — a quarter of the memory, and of the time that reading takes, for long contexts. Four calls:
+ * lilicorr_qk_norm_rope4 writes it, lilicorr_window_attention4 reads it, lilicorr_key_weights adds up how much
+ * attention every key has got, lilicorr_evict keeps the keys that count. Places, tables, starts and totals
+ * are lilicorr_page_plan's, and what is said above of the paged cache's calls holds for these.
+ *
+ * An element is E2M1 (a sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6), two to a byte, the even element in the low half. 32
+ * neighbouring elements of a head are a block with a scale byte b, 1 to 252: they stand for their values times
+ * 2^(b - 127). A block whose b is 255 is NaN throughout; 0, 253 and 254 are never written. Element x of head h of the token at place o of page p lies at byte
+ * p * page_stride + o * token_stride + h * head_stride + x / 2 of k (keys) and of v (values), its scale at a sixteenth
+ * of that offset (without x / 2) + x / 32 of k_scales and v_scales: scales are laid out as codes are.
+ */
+typedef struct {
+    void *k, *v;              /* codes, 16-byte aligned */
+    void *k_scales, *v_scales; /* bytes */
+    int page_size;
+    int heads;                /* key heads */
+    int d;                    /* head width: a multiple of 32, at most 256 */
+    int64_t pages;
+    int64_t page_stride, token_stride, head_stride; /* bytes of codes, multiples of 16 */
+} lilicorr_cache4;
+
+/*
+ * lilicorr_qk_norm_rope into a 4-bit cache. q, k, v, q_out of `dtype` (LILICORR_BF16 or LILICORR_F16); everything
+ * up to the rounding is as there. Of a block of k (normed and turned) or v (as it is), the scale is the least
+ * power of two s with max |x| <= 7 s, within 2^-126 .. 2^125, and each element the code nearest to x / s, ties to the
+ * even code, what is over 6 s to 6 s (so that no element is more than s off, short of the range's ends). Keys and
+ * their scales are those of the arithmetic in 64 bits. A block that holds an infinity or a NaN becomes NaN.
+ * Limits as for lilicorr_qk_norm_rope; the cache must not overlap q, k or v.
+ */
+typedef struct {
+    const void *q, *k, *v;
+    void *q_out;
+    lilicorr_cache4 cache;
+    const int32_t *slots, *positions;
+    const float *cos_sin, *q_weight, *k_weight;
+    int64_t q_stride, k_stride, v_stride, tokens, max_positions;
+    lilicorr_dtype dtype;
+    int heads, rot, interleaved;
+    float eps;
+} lilicorr_qk_norm_rope4_args;
+
+lilicorr_status lilicorr_qk_norm_rope4(const lilicorr_qk_norm_rope4_args *args, hipStream_t stream);
+
+/*
+ * lilicorr_window_attention over a 4-bit cache: the same queries, keys, masks, bounds, workspace rules and limits.
+ * q and out of `dtype`. Keys and values count as what their codes stand for, without a further rounding; fp16
+ * queries too (as two bf16 terms). Scores, softmax and sums in fp32; probabilities are rounded to bf16 for the
+ * second product, whatever `dtype` is, and the output once more. A key that a query does not see has no effect on it,
+ * NaN blocks among them; a NaN block of values that it sees makes those 32 elements of its output NaN.
+ *   lse   [tokens][heads] fp32 or NULL: the natural logarithm of each row's sum of exponentials, log sum_j exp(scale
+ *         q . k_j), of the probabilities before they are rounded; -inf where it sees no key. For
+ *         lilicorr_key_weights. 4-byte aligned. Neither out nor lse may overlap q's rows or one another.
+ */
+typedef struct {
+    const void *q;                  /* [tokens][heads][d] */
+    void *out;                      /* [tokens][heads][d], contiguous */
+    float *lse;
+    lilicorr_cache4 cache;
+    const int32_t *table;           /* [N][table_width] */
+    const int32_t *starts, *totals; /* [N + 1], [N] */
+    void *workspace;
+    size_t workspace_bytes;
+    int64_t tokens, q_stride;       /* q_stride: elements from token to token, a multiple of 8 */
+    int64_t N, table_width;
+    int64_t window, sinks;
+    int64_t max_tokens, max_length;
+    lilicorr_dtype dtype;
+    int heads, causal;
+    float scale;
+} lilicorr_attention4_args;
+
+/* Workspace bytes of the call (pointers are not looked at); 0 if the sizes are unsupported. */
+size_t lilicorr_window_attention4_workspace_bytes(const lilicorr_attention4_args *args);
+lilicorr_status lilicorr_window_attention4(const lilicorr_attention4_args *args, hipStream_t stream);
+
+/*
+ * Accumulated attention weight: how much of its probability every key has got from the queries of all steps so far.
+ * For every request n with T = starts[n+1] - starts[n] > 0 queries, and each of its keys j < totals[n] and cache heads h,
+ *   weights[j][h] = decay * before + sum over its queries t that see j, and the query heads g of h, of
+ *                   exp(scale q[t][g] . k[j][h] - lse[t][g]),
+ * where before is weights[j][h] for the keys j < totals[n] - T of earlier steps and 0 for the step's own keys (so that a
+ * page needs no clearing when it changes hands). Without a window: query t sees keys up to its own when
+ * `causal`, else all. Requests without queries, and keys on pages that are not there, are left as they are.
+ *   weights  [pages][cache heads][page_size] fp32, contiguous, 16-byte aligned: the places of the cache's pages.
+ *   lse      [tokens][heads] fp32 as lilicorr_window_attention4 gives it for the same queries and keys, without a
+ *            window; rows of -inf add nothing. 4-byte aligned.
+ *   cache    v and v_scales are not read, and may be NULL.
+ *   max_tokens, max_length   as for the attention: keys past max_length are left as they are, and so are requests with
+ *            more than max_tokens queries.
+ * In fp32 throughout. Each weight is added up by one wave in a fixed order, so the result is the same on every call. No two
+ * requests may share a page. decay finite and >= 0. Limits as for the attention.
+ */
+typedef struct {
+    const void *q;                  /* [tokens][heads][d] */
+    const float *lse;
+    float *weights;
+    lilicorr_cache4 cache;
+    const int32_t *table;           /* [N][table_width] */
+    const int32_t *starts, *totals; /* [N + 1], [N] */
+    int64_t tokens, q_stride;
+    int64_t N, table_width;
+    int64_t max_tokens, max_length;
+    lilicorr_dtype dtype;
+    int heads, causal;
+    float scale, decay;
+} lilicorr_key_weights_args;
+
+lilicorr_status lilicorr_key_weights(const lilicorr_key_weights_args *args, hipStream_t stream);
+
+/*
+ * Eviction by accumulated weight. Request n holds L = min(totals[n], pages[n][0] * page_size, table_width * page_size,
+ * max_length) tokens. One that holds more than `limit` is cut to `budget`: every cache head for itself keeps the
+ * first `sinks` tokens, the last `recent` ones, and of those between the budget - sinks - recent with the
+ * largest weights, the earlier one of equal weights (fp32 values in their order, -0 equal to 0; NaN above infinity, with
+ * the sign bit below all others). Kept tokens, keys, values, scales and weights, move to the places 0 .. budget - 1 of
+ * the request in their order; what its other places hold is left as it is. Different heads keep different tokens, so
+ * what is left has no common positions: use it without a window, and give new tokens the positions that they would have had
+ * (`evicted` more than lilicorr_page_plan says). The request's pages past the first ceil(budget / page_size) go to
+ * the end of the queue, as in lilicorr_page_plan. Other requests are left as they are. Nothing else may
+ * use the cache, the table or the queue at the time; no two requests may share a page.
+ *   totals [N], pages [N][2], table, queue, cursor   as lilicorr_page_plan has them after a step without a window.
+ *   totals_out [N]: L, or budget; pages_out [N][2], cursor_out [3] (the third as it is): for the next page plan.
+ *   evicted [N] int32: tokens that the request lost, L - totals_out[n].
+ *   weights  as for lilicorr_key_weights.
+ * Tokens on a page that is not there (outside [0, pages)) are the first to go and move nowhere. Outputs must not overlap
+ * inputs or one another; queue and weights are updated in place. workspace: scratch as for the attentions.
+ * Limits: 1 <= budget <= limit, sinks + recent <= budget; N <= 4096; otherwise as for the attention.
+ */
+typedef struct {
+    lilicorr_cache4 cache;
+    float *weights;
+    const int32_t *table, *totals, *pages;
+    int32_t *queue;
+    const int64_t *cursor;
+    int32_t *totals_out, *pages_out, *evicted;
+    int64_t *cursor_out;
+    void *workspace;
+    size_t workspace_bytes;
+    int64_t N, table_width, queue_size, max_length, budget, limit, sinks, recent;
+} lilicorr_evict_args;
+
+size_t lilicorr_evict_workspace_bytes(const lilicorr_evict_args *args);
+lilicorr_status lilicorr_evict(const lilicorr_evict_args *args, hipStream_t stream);
+
 /* Static, human-readable name of a status code. */
 const char *lilicorr_status_string(lilicorr_status s);
 

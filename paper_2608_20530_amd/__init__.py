@@ -24,6 +24,13 @@ Around the path, over a paged cache (paged.py):
   lilicorr_window_attention   paged attention with a sliding window and visible first tokens
   lilicorr_prefix_attention   paged attention of a batch that shares a long prefix
 
+The same cache in 4 bits, for long contexts (paged4.py):
+
+  lilicorr_qk_norm_rope4      head norms, rotation, keys and values into the cache in 4 bits
+  lilicorr_window_attention4  attention over it, and the logarithm of each row's sum
+  lilicorr_key_weights        the attention weight that every key has got so far
+  lilicorr_evict              each cache head keeps the heaviest keys; pages come back
+
 This module only marshals arguments: torch supplies device memory and the current HIP stream,
 and every step of the path runs in the library's kernels. There is no fallback: if the library
 is missing or fails to load, every call raises.
@@ -142,6 +149,7 @@ def load_library() -> ctypes.CDLL:
         "lilicorr_status_string": ([I], ctypes.c_char_p),
     }
     sig.update(paged.SIGNATURES)
+    sig.update(paged4.SIGNATURES)
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -815,4 +823,7 @@ def scorer_forward(X: torch.Tensor, packed: torch.Tensor, S: int, K: int, heads:
 from . import paged  # noqa: E402  (needs the names above)
 from .paged import *  # noqa: E402,F401,F403
 
-__all__ += paged.__all__
+from . import paged4  # noqa: E402
+from .paged4 import *  # noqa: E402,F401,F403
+
+__all__ += paged.__all__ + paged4.__all__

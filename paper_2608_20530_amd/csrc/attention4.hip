@@ -1,0 +1,289 @@
+// lilicorr_window_attention4 and lilicorr_key_weights: checks, tiles and chunks, launches.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "attention4.hpp"
+#include "cache4.hpp"
+#include "common.hpp"
+#include "lilicorr.h"
+#include "paged.hpp"
+
+namespace lilicorr {
+namespace {
+
+constexpr size_t kLeastBytes4 = 256;  // of a workspace
+// The longest sequences have so many tokens: lengths, windows and sinks past it say "without end"
+constexpr int64_t kMost4 = (int64_t)1 << 30;
+int64_t bounded4(int64_t n) { return n < kMost4 ? n : kMost4; }
+
+struct Plan4 {
+  int BM, tiles, chunk, chunks;  // rows of a tile; row tiles; 32-key tiles of a chunk; chunks
+  bool fast, spread;
+  int64_t rows;
+  size_t bytes;  // of the workspace
+};
+
+// Calls `use` with the kernel of a width and tile height. Up to 64 rows the waves share the keys, and a wave has all the
+// rows as long as they fit its registers; wider heads, and the two terms of fp16, leave room for fewer.
+template <typename T, int D, bool FAST, typename F>
+void with_rows4(int BM, const F& use) {
+  if (BM == 16) return use(Attn4Config<T, D, 1, 1, 4, FAST>());
+  if constexpr (D > 128) {
+    if (BM == 32) return use(Attn4Config<T, D, 1, 2, 2, FAST>());
+    return use(Attn4Config<T, D, 1, 4, 1, FAST>());
+  } else {
+    if (BM == 32) return use(Attn4Config<T, D, 2, 1, 4, FAST>());
+    if constexpr (D <= 64 || Query<T>::kTerms == 1) {
+      if (BM == 64) return use(Attn4Config<T, D, 4, 1, 4, FAST>());
+    } else {
+      if (BM == 64) return use(Attn4Config<T, D, 2, 2, 2, FAST>());
+    }
+    return use(Attn4Config<T, D, 2, 4, 1, FAST>());
+  }
+}
+int tile_rows4(int64_t rows, int d) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || d > 128 ? 64 : 128; }
+
+template <typename T, typename F>
+void with_kernel4(int d, bool fast, int BM, const F& use) {
+  auto width = [&](auto f) {
+    constexpr bool FAST = decltype(f)::value;
+    if (d <= 64) with_rows4<T, 64, FAST>(BM, use);
+    else if (d <= 128) with_rows4<T, 128, FAST>(BM, use);
+    else with_rows4<T, 256, FAST>(BM, use);
+  };
+  if (fast) width(std::true_type());
+  else width(std::false_type());
+}
+
+// What both calls check: sizes, then (without a workspace's query) the strides' reach
+template <typename A>
+lilicorr_status sizes4(const A& a) {
+  if (const lilicorr_status s = cache4_sizes(a.cache)) return s;
+  if (a.dtype != LILICORR_BF16 && a.dtype != LILICORR_F16) return LILICORR_ERR_INVALID_ARG;
+  if (a.tokens < 0 || a.N < 1 || a.table_width < 1 || a.heads < 1 || a.max_tokens < 0 || a.max_length < 0 ||
+      a.q_stride < 0)
+    return LILICORR_ERR_INVALID_ARG;
+  if (a.heads % a.cache.heads) return LILICORR_ERR_INVALID_ARG;
+  if (!(a.scale > 0.f) || !isfinite(a.scale)) return LILICORR_ERR_INVALID_ARG;
+  if (a.heads > 65535 || a.N > (1 << 20) || a.tokens > kMost4 / a.heads || a.table_width > kMost4 / a.cache.page_size)
+    return LILICORR_ERR_UNSUPPORTED;
+  if (!stride_ok(a.q_stride)) return LILICORR_ERR_ALIGNMENT;
+  // 16 keys of a page are reached with 32-bit offsets
+  if (a.cache.token_stride >= (int64_t)1 << 27) return LILICORR_ERR_UNSUPPORTED;
+  return LILICORR_OK;
+}
+
+lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
+  if (const lilicorr_status s = sizes4(a)) return s;
+  if (a.window < 0 || a.sinks < 0 || (a.sinks > 0 && a.window == 0)) return LILICORR_ERR_INVALID_ARG;
+  const int64_t group = a.heads / a.cache.heads;
+  const int64_t max_tokens = a.max_tokens < a.tokens ? a.max_tokens : a.tokens;
+  p.rows = a.tokens * a.heads;
+  const int64_t own = max_tokens * group;
+  p.BM = tile_rows4(own, a.cache.d);
+  const int64_t tiles = own <= p.BM ? a.N : a.tokens * group / p.BM + a.N;
+  int64_t keys = a.table_width * a.cache.page_size;
+  if (a.max_length < keys) keys = a.max_length;
+  int64_t most = (keys + 31) / 32;
+  if (a.window) {
+    // a tile's queries see at most this many: from the first one's window to the last one itself, or to the request's
+    // last token; each of the two runs may begin and end inside a tile of 32
+    const int64_t tile_tokens = p.BM / group + 1;
+    const int64_t seen = bounded4(a.window) + (a.causal && tile_tokens < max_tokens ? tile_tokens : max_tokens);
+    const int64_t tiles32 = (seen + 31) / 32 + 1 + (bounded4(a.sinks) + 31) / 32;
+    if (tiles32 < most) most = tiles32;
+  }
+  if (most < 1) most = 1;
+  p.fast = a.cache.page_size % 16 == 0;
+  p.spread = own <= p.BM;
+  // chunks so that all compute units have work
+  const int64_t items = tiles * a.cache.heads, wk = p.BM <= 64 ? 4 : 1;
+  const int64_t want = 768;
+  int64_t chunks = items >= want ? 1 : want / items;
+  const int64_t fit = (most + 2 * wk - 1) / (2 * wk);
+  if (chunks > fit) chunks = fit;
+  if (chunks > 64) chunks = 64;
+  const int64_t chunk = (most + chunks - 1) / chunks;
+  chunks = (most + chunk - 1) / chunk;
+  if (tiles * chunks > 0x7fffffffll / a.cache.heads) return LILICORR_ERR_UNSUPPORTED;
+  p.tiles = (int)tiles;
+  p.chunk = (int)chunk;
+  p.chunks = (int)chunks;
+  p.bytes = kLeastBytes4;
+  if (chunks > 1) p.bytes += (size_t)chunks * p.rows * (16 + (size_t)a.cache.d * 4);
+  return LILICORR_OK;
+}
+
+template <typename A>
+Attn4Args common4(const A& x) {
+  Attn4Args a = {};
+  const lilicorr_cache4& c = x.cache;
+  a.q = (const uint16_t*)x.q;
+  a.k = (const unsigned char*)c.k; a.v = (const unsigned char*)c.v;
+  a.ks = (const unsigned char*)c.k_scales; a.vs = (const unsigned char*)c.v_scales;
+  a.table = x.table; a.starts = x.starts; a.totals = x.totals;
+  a.q_stride = x.q_stride;
+  a.head_stride = c.head_stride; a.page_stride = c.page_stride; a.token_stride = c.token_stride;
+  a.rows = x.tokens * x.heads;
+  a.N = (int)x.N; a.pages = (int)c.pages; a.page_size = (uint32_t)c.page_size; a.table_width = (int)x.table_width;
+  divide_by(c.page_size, a.page_mul, a.page_shift);
+  a.tokens = (int)x.tokens; a.heads = x.heads; a.kv_heads = c.heads; a.group = x.heads / c.heads; a.d = c.d;
+  a.max_tokens = (int)(x.max_tokens < x.tokens ? x.max_tokens : x.tokens);
+  a.max_length = (int)bounded4(x.max_length);
+  a.causal = x.causal != 0;
+  a.scale2 = x.scale * 1.4426950408889634f;
+  return a;
+}
+
+template <typename C>
+void launch4(const Attn4Args& a, hipStream_t stream) {
+  if constexpr (C::kLds > 65536) {
+    static const hipError_t attr =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(attention4_kernel<C>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::kLds);
+    (void)attr;
+  }
+  hipLaunchKernelGGL(attention4_kernel<C>, dim3((unsigned)a.items), dim3(C::kThreads), C::kLds, stream, a);
+}
+
+template <typename T, int LPR>
+void launch_join4(const Attn4Args& a, int slots, hipStream_t stream) {
+  constexpr int64_t per = kJoin4Threads / kWave;
+  hipLaunchKernelGGL((attention4_join_kernel<T, LPR>), dim3((unsigned)((a.rows + per - 1) / per)), dim3(kJoin4Threads), 0,
+                     stream, a, slots);
+}
+
+template <typename T>
+lilicorr_status run4(const lilicorr_attention4_args& x, const Plan4& p, hipStream_t stream) {
+  Attn4Args a = common4(x);
+  a.out = (uint16_t*)x.out;
+  a.lse = x.lse;
+  a.window = (int)bounded4(x.window);
+  a.sinks = (int)bounded4(x.sinks);
+  a.tiles = p.tiles; a.chunk = p.chunk; a.most = p.chunk * p.chunks;
+  a.items = p.tiles * p.chunks * a.kv_heads;
+  a.spread = p.spread;
+  a.split = p.chunks > 1;
+  a.part_o = (float*)x.workspace;
+  a.part_ml = (f32x4_t*)((unsigned char*)x.workspace + (size_t)p.chunks * p.rows * a.d * 4);
+  with_kernel4<T>(a.d, p.fast, p.BM, [&](auto c) { launch4<decltype(c)>(a, stream); });
+  if (a.split) {
+    if (a.d <= 64) launch_join4<T, 16>(a, p.chunks, stream);
+    else if (a.d <= 128) launch_join4<T, 32>(a, p.chunks, stream);
+    else launch_join4<T, 64>(a, p.chunks, stream);
+  }
+  return launch_status();
+}
+
+// keys of a tile of key_weights_many_kernel: WK waves of 64
+template <typename T, bool FAST>
+void launch_weights(Attn4Args a, int d, hipStream_t stream) {
+  const bool few = (int64_t)a.max_tokens * a.group <= 16;
+  int64_t keys = (int64_t)a.table_width * a.page_size;
+  if (a.max_length < keys) keys = a.max_length;
+  if (keys < 1) return;
+  auto run = [&](auto width) {
+    constexpr int D = decltype(width)::value;
+    if (few) {
+      typedef Attn4Config<T, D, 1, 1, 4, FAST> C;
+      const int64_t most = (keys + 31) / 32, items = (int64_t)a.N * a.kv_heads, want = 1024;
+      int64_t chunks = items >= want ? 1 : want / items;
+      const int64_t fit = (most + 7) / 8;
+      if (chunks > fit) chunks = fit;
+      a.tiles = a.N;
+      a.chunk = (int)((most + chunks - 1) / chunks);
+      chunks = (most + a.chunk - 1) / a.chunk;
+      a.items = (int)(items * chunks);
+      a.spread = 1;
+      hipLaunchKernelGGL(key_weights_few_kernel<C>, dim3((unsigned)a.items), dim3(C::kThreads), 0, stream, a);
+    } else {
+      const int64_t groups = (keys + 63) / 64;
+      // enough key groups: neighbouring ones share the rows that they read; else the waves share the rows
+      if (groups * a.N * a.kv_heads >= 2048) {
+        typedef Attn4Config<T, D, 1, 1, 4, FAST> C;
+        a.tiles = (int)((groups + 3) / 4);
+        hipLaunchKernelGGL(key_weights_many_kernel<C>, dim3((unsigned)((int64_t)a.tiles * a.N * a.kv_heads)),
+                           dim3(C::kThreads), 0, stream, a);
+      } else {
+        typedef Attn4Config<T, D, 1, 4, 1, FAST> C;
+        a.tiles = (int)groups;
+        hipLaunchKernelGGL(key_weights_many_kernel<C>, dim3((unsigned)((int64_t)a.tiles * a.N * a.kv_heads)),
+                           dim3(C::kThreads), 0, stream, a);
+      }
+    }
+  };
+  if (d <= 64) run(std::integral_constant<int, 64>());
+  else if (d <= 128) run(std::integral_constant<int, 128>());
+  else run(std::integral_constant<int, 256>());
+}
+
+template <typename T>
+lilicorr_status run_weights(const lilicorr_key_weights_args& x, hipStream_t stream) {
+  Attn4Args a = common4(x);
+  a.lse_in = x.lse;
+  a.weights = x.weights;
+  a.decay = x.decay;
+  if (x.cache.page_size % 16 == 0) launch_weights<T, true>(a, a.d, stream);
+  else launch_weights<T, false>(a, a.d, stream);
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace lilicorr
+
+using namespace lilicorr;
+
+extern "C" size_t lilicorr_window_attention4_workspace_bytes(const lilicorr_attention4_args* args) {
+  Plan4 p;
+  return args && make_plan4(*args, p) == LILICORR_OK ? p.bytes : 0;
+}
+
+extern "C" lilicorr_status lilicorr_window_attention4(const lilicorr_attention4_args* args, hipStream_t stream) {
+  if (!args) return LILICORR_ERR_INVALID_ARG;
+  const lilicorr_attention4_args& x = *args;
+  Plan4 p;
+  if (const lilicorr_status s = make_plan4(x, p)) return s;
+  if (x.tokens == 0) return LILICORR_OK;
+  const lilicorr_cache4& c = x.cache;
+  if (!x.q || !x.out || !c.k || !c.v || !c.k_scales || !c.v_scales || !x.table || !x.starts || !x.totals || x.q == x.out)
+    return LILICORR_ERR_INVALID_ARG;
+  if (!aligned16(x.q) || !aligned16(x.out) || !aligned16(c.k) || !aligned16(c.v) || !aligned16(x.workspace) ||
+      !aligned4(x.lse) || !aligned4(x.table) || !aligned4(x.starts) || !aligned4(x.totals))
+    return LILICORR_ERR_ALIGNMENT;
+  if (!x.workspace || x.workspace_bytes < p.bytes) return LILICORR_ERR_WORKSPACE;
+  if (x.max_tokens == 0) return LILICORR_OK;
+  const size_t row = (size_t)x.heads * c.d * 2, out = row * (size_t)x.tokens;
+  const size_t lse = x.lse ? (size_t)x.heads * (size_t)x.tokens * 4 : 0;
+  if (rows_overlap(x.q, x.q_stride * 2, row, x.tokens, x.out, out) || overlap(x.out, out, x.lse, lse) ||
+      (lse && rows_overlap(x.q, x.q_stride * 2, row, x.tokens, x.lse, lse)))
+    return LILICORR_ERR_INVALID_ARG;
+  return x.dtype == LILICORR_BF16 ? run4<Bf16>(x, p, stream) : run4<F16>(x, p, stream);
+}
+
+extern "C" lilicorr_status lilicorr_key_weights(const lilicorr_key_weights_args* args, hipStream_t stream) {
+  if (!args) return LILICORR_ERR_INVALID_ARG;
+  const lilicorr_key_weights_args& x = *args;
+  if (const lilicorr_status s = sizes4(x)) return s;
+  if (!(x.decay >= 0.f) || !isfinite(x.decay)) return LILICORR_ERR_INVALID_ARG;
+  const lilicorr_cache4& c = x.cache;
+  const int64_t keys = x.table_width * c.page_size < x.max_length ? x.table_width * c.page_size : x.max_length;
+  if ((keys + 63) / 64 * x.N > 0x7fffffffll / c.heads) return LILICORR_ERR_UNSUPPORTED;
+  if (x.tokens == 0) return LILICORR_OK;
+  if (!x.q || !x.lse || !x.weights || !c.k || !c.k_scales || !x.table || !x.starts || !x.totals)
+    return LILICORR_ERR_INVALID_ARG;
+  if (!aligned16(x.q) || !aligned16(c.k) || !aligned16(x.weights) || !aligned4(x.lse) || !aligned4(x.table) ||
+      !aligned4(x.starts) || !aligned4(x.totals))
+    return LILICORR_ERR_ALIGNMENT;
+  if (x.max_tokens == 0) return LILICORR_OK;
+  // what other waves still read must not lie where the weights do
+  const size_t row = (size_t)x.heads * c.d * 2, w = (size_t)c.pages * c.page_size * c.heads * 4;
+  const size_t span = cache4_span(c);
+  if (rows_overlap(x.q, x.q_stride * 2, row, x.tokens, x.weights, w) ||
+      overlap(x.lse, (size_t)x.heads * (size_t)x.tokens * 4, x.weights, w) || overlap(c.k, span, x.weights, w) ||
+      overlap(c.k_scales, cache4_scales(span), x.weights, w) ||
+      overlap(x.table, (size_t)x.N * x.table_width * 4, x.weights, w) ||
+      overlap(x.starts, ((size_t)x.N + 1) * 4, x.weights, w) || overlap(x.totals, (size_t)x.N * 4, x.weights, w))
+    return LILICORR_ERR_INVALID_ARG;
+  return x.dtype == LILICORR_BF16 ? run_weights<Bf16>(x, stream) : run_weights<F16>(x, stream);
+}

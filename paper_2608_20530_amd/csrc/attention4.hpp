@@ -1,0 +1,914 @@
+// Attention over the 4-bit paged cache (lilicorr_window_attention4) and the attention weight that its keys have got
+// (lilicorr_key_weights).
+//
+// A row is one query head of one token; the query heads of a key head are neighbours, so the rows of a request and key
+// head are its tokens' groups one after the other. A wave holds RT blocks of 16 rows and goes through tiles of 32
+// keys; no data passes through LDS until the waves that shared the keys join.
+//
+// 16 x 16 x 32 matrix instructions. The order of the summed index is free as long as both operands have the same, so
+// each operand is what a lane can load at once. Lane l is c = l % 16 and g = l / 16.
+//   Scores S^T[key][row] = K . Q^T. Lane (c, g) has of key c (and 16 + c) the g-th quarter of the head: with heads of
+//   128 that is one 16-byte load and one scale, eight conversions a product. The result leaves lane (c, g) with row c
+//   and the keys 4 g .. 4 g + 3 (and 16 more).
+//   Output O^T[dim][row] = V^T . P^T sums over keys, of which lane (c, g) has just those eight probabilities. So it
+//   loads of the same eight keys the c-th sixteenth of the head, 4 bytes with heads of 128: after conversion a pair of
+//   neighbouring elements of one key, two v_perm bring two keys' elements together. Product i of D / 16
+//   has element i of every sixteenth, so a lane ends with whole runs of its row's output: D / 4 elements at D / 4 g.
+// Converted elements are exact in bf16, scale and all.
+//
+// Softmax: running maximum and sum in fp32, as in the 16-bit cache's attention: powers of two against a reference that
+// is a whole number and follows the maximum only when that has grown by more than 2^8. Probabilities go to the second product
+// rounded to bf16, and with fp16 outputs as two bf16 terms (with one, a ragged batch was 0.001 off, five times what the
+// output's own rounding is). The output's sum is that of the rounded probabilities (weights add up to one), the
+// logarithm's that of the unrounded ones.
+//
+// NaN blocks of values: 0 * NaN is NaN, so where not all rows see a key, its NaN blocks become zeros for the product
+// and the rows that do see it are marked, block by block, and get their NaN at the end.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cache4.hpp"
+#include "common.hpp"
+#include "paged.hpp"
+
+namespace lilicorr {
+namespace {
+
+typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4_t;
+
+constexpr float kRescale4 = 8.f;  // growth of the maximum, in powers of two, that is let pass
+
+// the largest of three; a NaN counts only beside NaNs
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  __asm__("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+struct Attn4Args {
+  const uint16_t* q;
+  const unsigned char *k, *v, *ks, *vs;
+  uint16_t* out;
+  float* lse;
+  float* part_o;     // [slots][tokens * heads][d], where the keys are split
+  f32x4_t* part_ml;  // [slots][tokens * heads]: maximum (powers of two), sums of rounded and unrounded powers
+  const int32_t *table, *starts, *totals;
+  int64_t q_stride, rows;  // rows = tokens * heads
+  int64_t head_stride;     // bytes
+  int N, pages, table_width;
+  uint32_t page_mul, page_shift, page_size;  // n / page_size = (n * page_mul) >> page_shift
+  int tokens, heads, kv_heads, group, d;
+  int64_t page_stride, token_stride;  // bytes
+  int tiles, chunk, most, items;      // row tiles; 32-key tiles of a chunk, and of all; tiles * heads * chunks
+  int spread, split;
+  int max_tokens, max_length, window, sinks, causal;
+  float scale2;  // scale * log2 e
+  // lilicorr_key_weights
+  const float* lse_in;
+  float* weights;
+  float decay;
+};
+
+template <typename T_, int D_, int RT_, int WR_, int WK_, bool FAST_>
+struct Attn4Config {
+  typedef T_ T;
+  static constexpr int D = D_;    // heads of D elements or fewer
+  static constexpr int RT = RT_;  // blocks of 16 rows of a wave
+  static constexpr int WR = WR_, WK = WK_;  // waves of rows by waves of keys
+  static constexpr bool FAST = FAST_;  // pages of a multiple of 16 tokens: 16 keys in one place
+  static constexpr int kWaves = WR * WK, kThreads = kWaves * kWave;
+  static constexpr int BM = 16 * RT * WR;
+  static constexpr int ND = D / 16;  // output products
+  static constexpr int KW = D / 32;  // 32-bit words that a lane has of a key
+  static constexpr int KS = D <= 128 ? 1 : 2;  // scales of them
+  static constexpr int VB = D / 32;  // bytes that a lane has of a value
+  static constexpr int kTerms = Query<T>::kTerms;
+  // the waves' partial outputs, in the order of their lanes, and sums
+  static constexpr uint32_t kOut = kWaves * RT * ND * kWave * 16, kSums = kWaves * RT * kWave * 16;
+  static constexpr uint32_t kLds = WK > 1 ? kOut + kSums : 0;
+};
+
+// What a wave has under way of a tile of 32 keys
+template <typename C>
+struct Raw4 {
+  uint32_t k[2][C::KW], ks[2][C::KS];
+  uint32_t v[8][C::VB > 4 ? 2 : 1], vs[8];
+};
+
+__device__ __forceinline__ int entry4(const Attn4Args& a, int j) {
+  return (int)(((uint64_t)(uint32_t)j * a.page_mul) >> a.page_shift);
+}
+
+// Where a wave's lanes find a tile's keys. `page` (one register) is the page of key lane % 32 of the tile, asked for
+// a tile ahead. FAST: two uniform bases, and offsets that a lane keeps; otherwise each key's own.
+template <typename C>
+struct Places4 {
+  uint32_t k_lane, v_lane;    // bytes of a lane's part within a key's, a value's codes
+  uint32_t k_scale, k_scale2, v_scale;  // and within its scales
+  uint32_t k_off, v_off;      // FAST: the same with the lane's (first) key
+  uint32_t ks_off, vs_off;
+
+  __device__ __forceinline__ void set(const Attn4Args& a) {
+    const int lane = lane_id(), c = lane & 15, g = lane >> 4;
+    // past the width of the head: its first part, which meets zeros of the queries, or goes to no output
+    const int ke = g * (C::D / 4), ve = c * (C::D / 16);
+    k_lane = ke < a.d ? ke / 2 : 0;
+    k_scale = ke < a.d ? ke / kBlock4 : 0;
+    k_scale2 = ke + kBlock4 < a.d ? ke / kBlock4 + 1 : 0;
+    v_lane = ve < a.d ? ve / 2 : 0;
+    v_scale = ve < a.d ? ve / kBlock4 : 0;
+    const uint32_t ts = (uint32_t)a.token_stride;
+    k_off = c * ts + k_lane;
+    v_off = 4 * g * ts + v_lane;
+    ks_off = c * (ts / 16) + k_scale;
+    vs_off = 4 * g * (ts / 16) + v_scale;
+  }
+};
+
+template <int BYTES>
+__device__ __forceinline__ void load_bytes(const unsigned char* p, uint32_t* to) {
+  if constexpr (BYTES == 2) {
+    to[0] = *reinterpret_cast<const uint16_t*>(p);
+  } else if constexpr (BYTES == 4) {
+    to[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (BYTES == 8) {
+    const u32x2_t w = *reinterpret_cast<const u32x2_t*>(p);
+    to[0] = w[0];
+    to[1] = w[1];
+  } else {
+    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(p);
+    to[0] = w[0];
+    to[1] = w[1];
+    to[2] = w[2];
+    to[3] = w[3];
+  }
+}
+
+// a lane's part of a key; the second half of a wide one lies 16 bytes on, or is the head's first where that ends
+template <typename C>
+__device__ __forceinline__ void load_key(const unsigned char* at, bool more, uint32_t* to) {
+  if constexpr (C::D <= 128) {
+    load_bytes<C::D / 8>(at, to);
+  } else {
+    load_bytes<16>(at, to);
+    load_bytes<16>(more ? at + 16 : at, to + 4);
+  }
+}
+
+// asks for the keys (and with VALUES the values) of a tile of 32
+template <typename C, bool VALUES>
+__device__ __forceinline__ void load4(const Attn4Args& a, const Places4<C>& pl, const unsigned char* k,
+                                      const unsigned char* v, const unsigned char* ks, const unsigned char* vs,
+                                      int tile, int page, Raw4<C>& r) {
+  const int lane = lane_id(), c = lane & 15, g = lane >> 4;
+  const bool more = g * (C::D / 4) + kBlock4 < a.d;
+  if constexpr (C::FAST) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int j = tile * 32 + h * 16;
+      const int p = (int)readlane32((uint32_t)page, h * 16);
+      const uint64_t base = (uint64_t)p * (uint64_t)a.page_stride +
+                            (uint64_t)((uint32_t)j - (uint32_t)entry4(a, j) * a.page_size) * (uint64_t)a.token_stride;
+      const unsigned char *kb = k + base, *vb = v + base, *kt = ks + base / 16, *vt = vs + base / 16;
+      load_key<C>(kb + pl.k_off, more, r.k[h]);
+      r.ks[h][0] = kt[pl.ks_off];
+      if constexpr (C::KS > 1) r.ks[h][1] = kt[pl.ks_off - pl.k_scale + pl.k_scale2];
+      if constexpr (VALUES) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          load_bytes<C::VB>(vb + e * a.token_stride + pl.v_off, r.v[4 * h + e]);
+          r.vs[4 * h + e] = (vt + e * (a.token_stride / 16))[pl.vs_off];
+        }
+      }
+    }
+  } else {
+    const int j = tile * 32 + (lane & 31);
+    const uint64_t mine = (uint64_t)(uint32_t)page * (uint64_t)a.page_stride +
+                          (uint64_t)((uint32_t)j - (uint32_t)entry4(a, j) * a.page_size) * (uint64_t)a.token_stride;
+    const uint32_t lo = (uint32_t)(mine >> 4), hi = (uint32_t)(mine >> 36);  // in 16 bytes
+    auto of = [&](int key) {
+      const uint32_t x = (uint32_t)__builtin_amdgcn_ds_bpermute(key * 4, (int)lo);
+      const uint32_t y = (uint32_t)__builtin_amdgcn_ds_bpermute(key * 4, (int)hi);
+      return (uint64_t)y << 32 | x;
+    };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint64_t at = of(16 * h + c);
+      load_key<C>(k + (at << 4) + pl.k_lane, more, r.k[h]);
+      r.ks[h][0] = ks[at + pl.k_scale];
+      if constexpr (C::KS > 1) r.ks[h][1] = ks[at + pl.k_scale2];
+      if constexpr (VALUES) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint64_t to = of(16 * h + 4 * g + e);
+          load_bytes<C::VB>(v + (to << 4) + pl.v_lane, r.v[4 * h + e]);
+          r.vs[4 * h + e] = vs[to + pl.v_scale];
+        }
+      }
+    }
+  }
+}
+
+// the h-th half's 16 keys as operands of the D / 32 score products
+template <typename C>
+__device__ __forceinline__ void keys4(const Raw4<C>& r, int h, u32x4_t (&to)[C::KW]) {
+#pragma unroll
+  for (int w = 0; w < C::KW; ++w) {
+    const uint32_t b = r.ks[h][C::KS > 1 ? w / 4 : 0];
+    const float s = scale_of(b);
+    const uint32_t x = r.k[h][w];
+    to[w] = u32x4_t{from4<0>(x, s), from4<1>(x, s), from4<2>(x, s), from4<3>(x, s)};
+  }
+}
+
+// elements 2 B and 2 B + 1 of the lane's part of its eight values, as operands
+template <typename C, int B>
+__device__ __forceinline__ void values4(const Raw4<C>& r, const float (&s)[8], u32x4_t& even, u32x4_t& odd) {
+  uint32_t p[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[e] = from4<B % 4>(r.v[e][B / 4], s[e]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    even[i] = __builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x05040100u);
+    odd[i] = __builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x07060302u);
+  }
+}
+
+// A wave's row of queries as operands of the score products: elements D / 4 g .. of row `at`, zeros past the width
+template <typename C>
+__device__ __forceinline__ void queries4(const uint16_t* at, int d, u32x4_t (&q)[C::kTerms][C::KW]) {
+  const int g = lane_id() >> 4;
+#pragma unroll
+  for (int w = 0; w < C::KW; ++w) {
+    const int x = g * (C::D / 4) + w * 8;
+    const u32x4_t in = x < d ? *reinterpret_cast<const u32x4_t*>(at + x) : u32x4_t{0, 0, 0, 0};
+    u32x4_t t[C::kTerms];
+    Query<typename C::T>::split(in, t);
+#pragma unroll
+    for (int i = 0; i < C::kTerms; ++i) q[i][w] = t[i];
+  }
+}
+
+// Which rows a tile of BM has: request n, its first row r0 and the end r1 of them, first token, position of the first
+// query. False where there are none.
+struct Rows4 {
+  int n, r0, r1, start, T, total, pos0;
+};
+template <int BM>
+__device__ __forceinline__ bool rows4(const Attn4Args& a, int tile, Rows4& r) {
+  auto starts_at = [&](int i) { return min(max(a.starts[i], 0), a.tokens); };
+  int n = 0;
+  if ((int64_t)a.max_tokens * a.group <= BM) {
+    n = tile;
+    r.r0 = 0;
+  } else {
+    // request n's tiles have the numbers floor(starts[n] * group / BM) + n and on, which is at least as many as it
+    // has; 64 candidates at a time
+    auto first_tile = [&](int i) { return (int)((int64_t)starts_at(i) * a.group / BM) + i; };
+    int end = a.N;
+    while (end - n > 1) {
+      const int step = (end - n + kWave - 1) / kWave, i = n + lane_id() * step;
+      const uint64_t le = __ballot(i < end && first_tile(i) <= tile);
+      const int last = 63 - __builtin_clzll(le | 1);
+      n += last * step;
+      end = min(end, n + step);
+    }
+    n = (int)uniform32(n);
+    r.r0 = (tile - first_tile(n)) * BM;
+  }
+  r.n = n;
+  r.start = starts_at(n);
+  r.T = starts_at(n + 1) - r.start;
+  r.total = max(a.totals[n], 0);
+  r.pos0 = r.total - r.T;
+  const int T = min(r.T, a.max_tokens);
+  if (r.r0 < 0 || r.r0 >= (int64_t)T * a.group) return false;
+  r.r1 = (int)min((int64_t)T * a.group, (int64_t)r.r0 + BM);
+  return true;
+}
+
+template <typename C>
+__global__ __launch_bounds__(C::kThreads) void attention4_kernel(Attn4Args a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char attn4_smem[];
+  typedef typename C::T T;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wave = (int)uniform32(tid >> 6);
+  const int wr = wave % C::WR, wk = wave / C::WR;
+
+  // ---- which rows ------------------------------------------------------------------------------
+  int it = (int)blockIdx.x;
+  if (a.spread) {
+    const int per = a.items / 8;
+    if (it < per * 8) it = (it % 8) * per + it / 8;
+  }
+  const int head = it % a.kv_heads;
+  const int rest = it / a.kv_heads;
+  const int chunk_no = rest / a.tiles;
+  Rows4 rw;
+  // long rows first: with a causal mask and no window the last tiles of a request see most
+  if (!rows4<C::BM>(a, a.tiles - 1 - rest % a.tiles, rw)) return;
+  const int r0 = rw.r0, r1 = rw.r1;
+
+  // ---- which keys ------------------------------------------------------------------------------
+  const int p_lo = rw.pos0 + r0 / a.group, p_hi = rw.pos0 + (r1 - 1) / a.group;
+  int hi = a.causal ? min(rw.total, p_hi + 1) : rw.total;
+  hi = max((int)min((int64_t)min(hi, a.max_length), a.table_width * (int64_t)a.page_size), 0);
+  const int lo = a.window ? min(max(p_lo - a.window + 1, 0), hi) : 0;
+  const int ns = min(a.sinks, lo);
+  // tiles of 32 keys: those of the sinks, then those of the window, as one list
+  const int t_lo = lo / 32, s_t = min((ns + 31) / 32, t_lo);
+  const int nt = min(s_t + (hi + 31) / 32 - t_lo, a.most);
+  const int t_begin = chunk_no * a.chunk, t_end = min(nt, t_begin + a.chunk);
+
+  int row[C::RT], p[C::RT];
+  int64_t orow[C::RT];
+  u32x4_t q[C::RT][C::kTerms][C::KW];
+#pragma unroll
+  for (int t = 0; t < C::RT; ++t) {
+    row[t] = r0 + (wr * C::RT + t) * 16 + c;
+    const int rc = min(row[t], r1 - 1), tok = rc / a.group, hq = head * a.group + (rc - tok * a.group);
+    orow[t] = ((int64_t)rw.start + tok) * a.heads + hq;
+    p[t] = rw.pos0 + tok;
+    if (t_begin < t_end) queries4<C>(a.q + ((int64_t)rw.start + tok) * a.q_stride + (int64_t)hq * a.d, a.d, q[t]);
+  }
+  if (t_begin >= t_end && chunk_no > 0) {  // (chunk 0 of a tile without keys writes its zeros below)
+    if (wk == 0 && g == 0)
+#pragma unroll
+      for (int t = 0; t < C::RT; ++t)
+        if (row[t] < r1) a.part_ml[(int64_t)chunk_no * a.rows + orow[t]] = f32x4_t{-__builtin_inff(), 0.f, 0.f, 0.f};
+    return;
+  }
+  // the wave's rows: positions of its first and last
+  const int wrow0 = r0 + wr * C::RT * 16;
+  const int wp_lo = rw.pos0 + min(wrow0, r1 - 1) / a.group;
+  const int wp_hi = rw.pos0 + min(wrow0 + C::RT * 16 - 1, r1 - 1) / a.group;
+
+  Places4<C> pl;
+  pl.set(a);
+  const int64_t ho = (int64_t)head * a.head_stride;
+  const unsigned char *k = a.k + ho, *v = a.v + ho, *ks = a.ks + ho / 16, *vs = a.vs + ho / 16;
+  const int32_t* trow = a.table + (int64_t)rw.n * a.table_width;
+  auto tile_at = [&](int i) { return i < s_t ? i : i - s_t + t_lo; };
+  auto page_of = [&](int i) {  // of key lane % 32 of the list's tile i, or of the last one's last key
+    const int j = min(tile_at(min(i, t_end - 1)) * 32 + (lane & 31), hi - 1);
+    return trow[entry4(a, j)];
+  };
+
+  f32x4_t o[C::RT][C::ND];
+  float m[C::RT], l[C::RT], lu[C::RT];
+  uint32_t poison[C::RT];
+#pragma unroll
+  for (int t = 0; t < C::RT; ++t) {
+#pragma unroll
+    for (int i = 0; i < C::ND; ++i) o[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    m[t] = -__builtin_inff();
+    l[t] = lu[t] = 0.f;
+    poison[t] = 0;
+  }
+
+  // one tile, `page` its keys' pages as the table has them
+  auto use = [&](Raw4<C>& r, int i, int page) __attribute__((always_inline)) {
+    const int j0 = tile_at(i) * 32;
+    const uint32_t here = (uint32_t)__ballot(page >= 0 && page < a.pages) & bits32_below(hi - j0);
+    const bool whole = here == ~0u && (!a.causal || j0 + 31 <= wp_lo) &&
+                       (!a.window || j0 > wp_hi - a.window || j0 + 31 < a.sinks);
+    uint32_t vis[C::RT];
+    if (!whole) {
+#pragma unroll
+      for (int t = 0; t < C::RT; ++t) {
+        vis[t] = here;
+        if (a.causal) vis[t] &= bits32_below(p[t] + 1 - j0);
+        if (a.window) vis[t] &= bits32_from(p[t] - a.window + 1 - j0) | bits32_below(a.sinks - j0);
+      }
+    }
+    f32x4_t sc[C::RT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4_t kk[C::KW];
+      keys4<C>(r, h, kk);
+#pragma unroll
+      for (int t = 0; t < C::RT; ++t) {
+        sc[t][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < C::KW; ++w)
+#pragma unroll
+          for (int u = 0; u < C::kTerms; ++u) sc[t][h] = mfma16(kk[w], q[t][u][w], sc[t][h]);
+      }
+    }
+    u32x4_t pf[C::RT][C::kTerms];
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t) {
+      if (!whole) {
+        const uint32_t mine = vis[t] >> (4 * g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          sc[t][e / 4][e % 4] = mine & (1u << (16 * (e / 4) + e % 4)) ? sc[t][e / 4][e % 4] : -__builtin_inff();
+      }
+      float mx = max3(sc[t][0][0], sc[t][0][1], sc[t][0][2]);
+      mx = max3(mx, sc[t][0][3], sc[t][1][0]);
+      mx = max3(mx, sc[t][1][1], sc[t][1][2]);
+      mx = max3(mx, sc[t][1][3], mx);
+      // -inf - -inf is NaN and does not count
+      if (__ballot(fmaf(mx, a.scale2, -m[t]) > kRescale4)) {
+        mx = quad_max(mx);
+        const bool grows = fmaf(mx, a.scale2, -m[t]) > kRescale4;
+        const float up = __builtin_floorf(mx * a.scale2);
+        // nothing is accumulated while m is -inf
+        const float f = grows ? __builtin_amdgcn_ldexpf(1.f, (int)fmaxf(m[t] - up, -300.f)) : 1.f;
+        m[t] = grows ? up : m[t];
+        l[t] *= f;
+        lu[t] *= f;
+#pragma unroll
+        for (int i = 0; i < C::ND; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[t][i][e] *= f;
+      }
+      const float ms = m[t] == -__builtin_inff() ? 0.f : m[t];
+      float e[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        e[x] = __builtin_amdgcn_exp2f(fmaf(sc[t][x / 4][x % 4], a.scale2, -ms));
+        lu[t] += e[x];
+      }
+      typedef __bf16 pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t w = Bf16::pack(e[2 * x], e[2 * x + 1]);
+        pf[t][0][x] = w;
+        if constexpr (C::kTerms > 1) {
+          const f32x2_t hi = Bf16::unpack(w);
+          pf[t][1][x] = Bf16::pack(e[2 * x] - hi[0], e[2 * x + 1] - hi[1]);
+        } else {
+          l[t] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, 0x3f803f80u),
+                                                 l[t], false);
+        }
+      }
+    }
+    if (!whole) {  // NaN blocks of values
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, r.vs[e]);
+      if (__ballot(top > kMostScale)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint64_t bad = __ballot(r.vs[e] > kMostScale);
+#pragma unroll
+          for (int b = 0; b < C::D / kBlock4; ++b) {
+            // the first lane of each quarter that has elements of block b
+            const uint64_t of = bad >> (b * (512 / C::D));
+            const uint32_t keys = ((uint32_t)(of & 1) | ((uint32_t)(of >> 16 & 1) << 4) | ((uint32_t)(of >> 32 & 1) << 8) |
+                                   ((uint32_t)(of >> 48 & 1) << 12)) << (e < 4 ? e : 16 + e - 4);
+#pragma unroll
+            for (int t = 0; t < C::RT; ++t) poison[t] |= vis[t] & keys ? 1u << b : 0u;
+          }
+          if (r.vs[e] > kMostScale) {
+            r.vs[e] = 127;
+            r.v[e][0] = 0;
+            if constexpr (C::VB > 4) r.v[e][1] = 0;
+          }
+        }
+      }
+    }
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = scale_of(r.vs[e]);
+    auto product = [&](auto b) __attribute__((always_inline)) {
+      constexpr int B = decltype(b)::value;
+      u32x4_t even, odd;
+      values4<C, B>(r, s, even, odd);
+#pragma unroll
+      for (int t = 0; t < C::RT; ++t) {
+#pragma unroll
+        for (int u = 0; u < C::kTerms; ++u) {
+          o[t][2 * B] = mfma16(even, pf[t][u], o[t][2 * B]);
+          o[t][2 * B + 1] = mfma16(odd, pf[t][u], o[t][2 * B + 1]);
+        }
+      }
+    };
+    product(std::integral_constant<int, 0>{});
+    product(std::integral_constant<int, 1>{});
+    if constexpr (C::VB > 2) {
+      product(std::integral_constant<int, 2>{});
+      product(std::integral_constant<int, 3>{});
+    }
+    if constexpr (C::VB > 4) {
+      product(std::integral_constant<int, 4>{});
+      product(std::integral_constant<int, 5>{});
+      product(std::integral_constant<int, 6>{});
+      product(std::integral_constant<int, 7>{});
+    }
+  };
+  auto place = [&](int page) { return page >= 0 && page < a.pages ? page : 0; };
+  auto load = [&](int i, int page, Raw4<C>& r) __attribute__((always_inline)) {
+    load4<C, true>(a, pl, k, v, ks, vs, tile_at(min(i, t_end - 1)), place(page), r);
+  };
+  // two sets of registers in turn: a tile is asked for while the one before it is used, its pages a tile earlier
+  int i = t_begin + wk;
+  if (i < t_end) {
+    Raw4<C> ra, rb;
+    int pa = page_of(i), pb = page_of(i + C::WK);
+    load(i, pa, ra);
+    while (true) {
+      int next = page_of(i + 2 * C::WK);
+      load(i + C::WK, pb, rb);
+      use(ra, i, pa);
+      pa = next;
+      i += C::WK;
+      if (i >= t_end) break;
+      next = page_of(i + 2 * C::WK);
+      load(i + C::WK, pa, ra);
+      use(rb, i, pb);
+      pb = next;
+      i += C::WK;
+      if (i >= t_end) break;
+    }
+  }
+
+  // ---- join the waves that shared the keys ---------------------------------------------------------
+#pragma unroll
+  for (int t = 0; t < C::RT; ++t) {
+    lu[t] = quad_sum(lu[t]);
+    l[t] = C::kTerms > 1 ? lu[t] : quad_sum(l[t]);  // two terms of a probability round next to nothing
+    if (__ballot(poison[t] != 0)) {
+      // lane (c, g) has the elements D / 4 g + D / 16 r + i of its row, in o[t][i][r]
+#pragma unroll
+      for (int i = 0; i < C::ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (poison[t] >> ((g * (C::D / 4) + r * (C::D / 16)) / kBlock4) & 1) o[t][i][r] = __builtin_nanf("");
+    }
+  }
+  if constexpr (C::WK > 1) {
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t) {
+#pragma unroll
+      for (int i = 0; i < C::ND; ++i)
+        *(lds_f32x4_t)(attn4_smem + (((wave * C::RT + t) * C::ND + i) * kWave + lane) * 16) = o[t][i];
+      *(lds_f32x4_t)(attn4_smem + C::kOut + ((wave * C::RT + t) * kWave + lane) * 16) = f32x4_t{m[t], l[t], lu[t], 0.f};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t) {
+      f32x4_t ml[C::WK];
+      float f[C::WK], top = -__builtin_inff();
+#pragma unroll
+      for (int w = 0; w < C::WK; ++w) {
+        ml[w] = *(lds_f32x4_t)(attn4_smem + C::kOut + (((w * C::WR + wr) * C::RT + t) * kWave + lane) * 16);
+        top = fmaxf(top, ml[w][0]);
+      }
+      l[t] = lu[t] = 0.f;
+#pragma unroll
+      for (int w = 0; w < C::WK; ++w) {
+        f[w] = ml[w][0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[w][0] - top);
+        l[t] += f[w] * ml[w][1];
+        lu[t] += f[w] * ml[w][2];
+      }
+      m[t] = top;
+#pragma unroll
+      for (int i = 0; i < C::ND; ++i) {
+        if (i / (C::ND / C::WK) != wk) continue;  // each of the waves joins its share of the products
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < C::WK; ++w)
+          sum += f[w] * *(lds_f32x4_t)(attn4_smem + ((((w * C::WR + wr) * C::RT + t) * C::ND + i) * kWave + lane) * 16);
+        o[t][i] = sum;
+      }
+    }
+  }
+
+  // ---- write ---------------------------------------------------------------------------------------
+  constexpr int kMine = C::ND / C::WK;  // products that this wave writes: elements kMine wk .. of each run of ND
+#pragma unroll
+  for (int t = 0; t < C::RT; ++t) {
+    if (row[t] >= r1) continue;
+    const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];  // a row that sees nothing gives zeros
+    if (wk == 0 && g == 0) {
+      if (a.split) a.part_ml[(int64_t)chunk_no * a.rows + orow[t]] = f32x4_t{m[t], l[t], lu[t], 0.f};
+      else if (a.lse)
+        a.lse[orow[t]] = lu[t] == 0.f ? -__builtin_inff() : (m[t] + __builtin_amdgcn_logf(lu[t])) * 0.6931471805599453f;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int x = g * (C::D / 4) + r * C::ND + wk * kMine;
+      if (x >= a.d) continue;
+      float f[kMine];
+#pragma unroll
+      for (int i = 0; i < C::ND; ++i)
+        if (i / kMine == wk) f[i % kMine] = o[t][i][r];
+      if (a.split) {
+        float* to = a.part_o + ((int64_t)chunk_no * a.rows + orow[t]) * a.d + x;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) to[i] = f[i];
+      } else {
+        uint16_t* to = a.out + orow[t] * a.d + x;
+        if constexpr (kMine == 1) {
+          to[0] = (uint16_t)T::pack(f[0] * inv, 0.f);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kMine; i += 2)
+            *reinterpret_cast<uint32_t*>(to + i) = T::pack(f[i] * inv, f[i + 1] * inv);
+        }
+      }
+    }
+  }
+}
+
+// Joins the slots of every row in their order, a wave a row: maxima and sums one lane a slot, then the partial outputs
+// in 16 bytes a lane, LPR lanes a slot and 64 / LPR slots at once.
+constexpr int kJoin4Threads = 256;
+template <typename T, int LPR>
+__global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Args a, int slots) {
+  constexpr int kAtOnce = kWave / LPR;
+  const int lane = lane_id();
+  const int64_t row = (int64_t)blockIdx.x * (kJoin4Threads / kWave) + threadIdx.x / kWave;
+  const int x = (lane % LPR) * 4;
+  if (row >= a.rows) return;
+  const int64_t used = (int64_t)min(max(a.starts[a.N], 0), a.tokens) * a.heads;
+  float top = -__builtin_inff(), l = 0.f, lu = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < slots; s0 += kWave) {
+    const int here = min(slots - s0, kWave);
+    constexpr int kBatch = 8;
+    f32x4_t v[kBatch];
+    // a slot that saw nothing holds no output: read all the same, beside its sum, and not used
+    auto load = [&](int b) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int s = b + u * kAtOnce + lane / LPR;
+        v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (s < here && x < a.d)
+          v[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + ((s0 + s) * a.rows + row) * a.d + x);
+      }
+    };
+    f32x4_t ml = {-__builtin_inff(), 0.f, 0.f, 0.f};
+    if (lane < here) ml = a.part_ml[(s0 + lane) * a.rows + row];
+    load(0);
+    const float grown = fmaxf(top, wave_max_dpp(ml[0]));
+    const float f0 = top == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(top - grown);
+    // the sum of a slot that saw nothing is 0; a NaN stays one
+    const float f = ml[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[0] - grown);
+    const bool saw = ml[1] != 0.f;
+    top = grown;
+    l = l * f0 + wave_sum_dpp(saw ? f * ml[1] : 0.f);
+    lu = lu * f0 + wave_sum_dpp(saw ? f * ml[2] : 0.f);
+    o *= f0;
+    const uint64_t which = __ballot(saw);
+    for (int b = 0; b < here; b += kBatch * kAtOnce) {
+      if (b) load(b);
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int s = b + u * kAtOnce + lane / LPR;
+        const bool on = s < here && ((which >> (s & 63)) & 1);
+        const float w = __shfl(f, s & 63, kWave);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += on ? w * v[u][e] : 0.f;
+      }
+    }
+  }
+  if (row >= used) return;
+#pragma unroll
+  for (int m = LPR; m < kWave; m <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m, kWave);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (lane < LPR && x < a.d)
+    *reinterpret_cast<u32x2_t*>(a.out + row * a.d + x) =
+        u32x2_t{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
+  if (lane == 0 && a.lse)
+    a.lse[row] = lu == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(lu)) * 0.6931471805599453f;
+}
+
+// ---- accumulated weights ---------------------------------------------------------------------------
+
+// place of a key's weight
+__device__ __forceinline__ int64_t weight_at(const Attn4Args& a, int page, int head, int j) {
+  return ((int64_t)page * a.kv_heads + head) * a.page_size + (j - entry4(a, j) * (int)a.page_size);
+}
+
+// Requests with at most 16 rows: a wave goes through tiles of 32 keys as in the attention. The scores stand the
+// other way round, S[row][key], so that a lane has four rows of one key and the sum over rows is three
+// additions and two exchanges.
+template <typename C>
+__global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args a) {
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wk = (int)uniform32(tid >> 6);
+  int it = (int)blockIdx.x;
+  if (a.spread) {
+    const int per = a.items / 8;
+    if (it < per * 8) it = (it % 8) * per + it / 8;
+  }
+  const int head = it % a.kv_heads;
+  const int rest = it / a.kv_heads;
+  const int chunk_no = rest / a.tiles;
+  Rows4 rw;
+  if (!rows4<16>(a, rest % a.tiles, rw) || rw.T > a.max_tokens) return;
+  const int hi = max((int)min((int64_t)min(rw.total, a.max_length), a.table_width * (int64_t)a.page_size), 0);
+  const int t_begin = chunk_no * a.chunk, t_end = min((hi + 31) / 32, t_begin + a.chunk);
+  int i = t_begin + wk;
+  if (i >= t_end) return;
+
+  u32x4_t q[C::kTerms][C::KW];
+  {
+    const int rc = min(c, rw.r1 - 1), tok = rc / a.group, hq = head * a.group + (rc - tok * a.group);
+    queries4<C>(a.q + ((int64_t)rw.start + tok) * a.q_stride + (int64_t)hq * a.d, a.d, q);
+  }
+  float ls[4];  // of row 4 g + r; no row, or one that sees nothing: its powers are 0
+  int p[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int x = 4 * g + r, rc = min(x, rw.r1 - 1), tok = rc / a.group, hq = head * a.group + (rc - tok * a.group);
+    const float v = a.lse_in[((int64_t)rw.start + tok) * a.heads + hq];
+    ls[r] = x >= rw.r1 || v == -__builtin_inff() ? __builtin_inff() : v * 1.4426950408889634f;
+    p[r] = rw.pos0 + tok;
+  }
+  Places4<C> pl;
+  pl.set(a);
+  const int64_t ho = (int64_t)head * a.head_stride;
+  const unsigned char *k = a.k + ho, *ks = a.ks + ho / 16;
+  const int32_t* trow = a.table + (int64_t)rw.n * a.table_width;
+  auto page_of = [&](int x) {
+    const int j = min(min(x, t_end - 1) * 32 + (lane & 31), hi - 1);
+    return trow[entry4(a, j)];
+  };
+  auto place = [&](int page) { return page >= 0 && page < a.pages ? page : 0; };
+  auto load = [&](int x, int page, Raw4<C>& r, float& w) __attribute__((always_inline)) {
+    x = min(x, t_end - 1);
+    load4<C, false>(a, pl, k, k, ks, ks, x, place(page), r);
+    w = a.weights[weight_at(a, place(page), head, x * 32 + (lane & 31))];
+  };
+  auto use = [&](const Raw4<C>& r, float before, int x, int page) __attribute__((always_inline)) {
+    const int j0 = x * 32;
+    const bool all = !a.causal || j0 + 31 <= rw.pos0;
+    float got[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4_t kk[C::KW];
+      keys4<C>(r, h, kk);
+      f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < C::KW; ++w)
+#pragma unroll
+        for (int u = 0; u < C::kTerms; ++u) sc = mfma16(q[u][w], kk[w], sc);
+      float e[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        e[y] = __builtin_amdgcn_exp2f(ls[y] == __builtin_inff() ? -__builtin_inff() : fmaf(sc[y], a.scale2, -ls[y]));
+        if (!all) e[y] = j0 + 16 * h + c <= p[y] ? e[y] : 0.f;
+      }
+      got[h] = quad_sum((e[0] + e[1]) + (e[2] + e[3]));
+    }
+    const int j = j0 + lane;  // lanes 0 .. 31
+    if (lane < 32 && j < hi && page >= 0 && page < a.pages)
+      a.weights[weight_at(a, page, head, j)] = (j < rw.pos0 ? a.decay * before : 0.f) + (lane < 16 ? got[0] : got[1]);
+  };
+  Raw4<C> ra, rb;
+  float wa, wb;
+  int pa = page_of(i), pb = page_of(i + C::WK);
+  load(i, pa, ra, wa);
+  while (true) {
+    int next = page_of(i + 2 * C::WK);
+    load(i + C::WK, pb, rb, wb);
+    use(ra, wa, i, pa);
+    pa = next;
+    i += C::WK;
+    if (i >= t_end) break;
+    next = page_of(i + 2 * C::WK);
+    load(i + C::WK, pa, ra, wa);
+    use(rb, wb, i, pb);
+    pb = next;
+    i += C::WK;
+    if (i >= t_end) break;
+  }
+}
+
+// More rows: a wave keeps 64 keys as operands and goes through the rows that see them, 16 at a time; the
+// scores stand as in the attention, S^T[key][row], so that a row's logarithm is one register and the sum over rows waits for
+// the end. The workgroup's waves have the keys of WK neighbouring groups and WR shares of the rows.
+template <typename C>
+__global__ __launch_bounds__(C::kThreads) void key_weights_many_kernel(Attn4Args a) {
+  __shared__ float s_sum[C::kWaves][kWave];
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wave = (int)uniform32(tid >> 6), wr = wave % C::WR, wk = wave / C::WR;
+  const int head = (int)blockIdx.x % a.kv_heads;
+  const int rest = (int)blockIdx.x / a.kv_heads;
+  const int n = rest / a.tiles;
+  auto starts_at = [&](int i) { return min(max(a.starts[i], 0), a.tokens); };
+  const int start = starts_at(n), T = starts_at(n + 1) - start, total = max(a.totals[n], 0), pos0 = total - T;
+  const int hi = max((int)min((int64_t)min(total, a.max_length), a.table_width * (int64_t)a.page_size), 0);
+  const int j0 = ((rest % a.tiles) * C::WK + wk) * 64;
+  const bool any = T > 0 && T <= a.max_tokens && j0 < hi;
+  float acc[4][4];
+#pragma unroll
+  for (int h = 0; h < 4; ++h)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[h][r] = 0.f;
+  const int j = j0 + 16 * (c >> 2) + 4 * g + (c & 3);  // the key whose weight this lane writes
+  int my_page = -1;
+  if (any) {
+    const int32_t* trow = a.table + (int64_t)n * a.table_width;
+    u32x4_t kk[4][C::KW];
+    {
+      Places4<C> pl;
+      pl.set(a);
+      const int64_t ho = (int64_t)head * a.head_stride;
+      const unsigned char *k = a.k + ho, *ks = a.ks + ho / 16;
+      Raw4<C> r[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int key = min(j0 + 32 * x + (lane & 31), hi - 1);
+        const int page = trow[entry4(a, key)];
+        load4<C, false>(a, pl, k, k, ks, ks, min(j0 / 32 + x, (hi - 1) / 32), page >= 0 && page < a.pages ? page : 0, r[x]);
+      }
+      if (j < hi) my_page = trow[entry4(a, j)];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) keys4<C>(r[h >> 1], h & 1, kk[h]);
+    }
+    const int rows = T * a.group;
+    const int first = a.causal ? max(j0 - pos0, 0) * a.group / 16 * 16 : 0;  // of the rows that see the first key
+    u32x4_t qa[C::KW], qb[C::KW];
+    float la, lb;
+    int ta, tb;
+    auto load = [&](int r0, u32x4_t (&q)[C::KW], float& ls, int& tok) __attribute__((always_inline)) {
+      const int r = r0 + c, rc = min(r, rows - 1);
+      tok = rc / a.group;
+      const int hq = head * a.group + (rc - tok * a.group);
+      const uint16_t* at = a.q + ((int64_t)start + tok) * a.q_stride + (int64_t)hq * a.d;
+#pragma unroll
+      for (int w = 0; w < C::KW; ++w) {
+        const int x = g * (C::D / 4) + w * 8;
+        q[w] = x < a.d ? *reinterpret_cast<const u32x4_t*>(at + x) : u32x4_t{0, 0, 0, 0};
+      }
+      ls = a.lse_in[((int64_t)start + tok) * a.heads + hq];
+      if (r >= rows) ls = -__builtin_inff();
+    };
+    auto use = [&](const u32x4_t (&in)[C::KW], float v, int tok) __attribute__((always_inline)) {
+      // no row, or one that sees nothing: its powers are 0
+      const bool none = v == -__builtin_inff();
+      const float ls = v * 1.4426950408889634f;
+      const int p = pos0 + tok;
+      const bool all = !__ballot(none || (a.causal && p < j0 + 63));
+      u32x4_t q[C::KW][C::kTerms];
+#pragma unroll
+      for (int w = 0; w < C::KW; ++w) Query<typename C::T>::split(in[w], q[w]);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < C::KW; ++w)
+#pragma unroll
+          for (int u = 0; u < C::kTerms; ++u) sc = mfma16(kk[h][w], q[w][u], sc);
+        if (!all) {
+          const int last = none ? -1 : a.causal ? p - (j0 + 16 * h + 4 * g) : 4;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale2, -ls));
+            acc[h][r] += r <= last ? e : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[h][r] += __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale2, -ls));
+        }
+      }
+    };
+    int r0 = first + wr * 16;
+    if (r0 < rows) {
+      load(r0, qa, la, ta);
+      while (true) {
+        load(r0 + 16 * C::WR, qb, lb, tb);
+        use(qa, la, ta);
+        r0 += 16 * C::WR;
+        if (r0 >= rows) break;
+        load(r0 + 16 * C::WR, qa, la, ta);
+        use(qb, lb, tb);
+        r0 += 16 * C::WR;
+        if (r0 >= rows) break;
+      }
+    }
+  }
+  // the sum over the 16 lanes' rows; lane (c, g) takes key 16 (c / 4) + 4 g + c % 4
+  float got = 0.f;
+#pragma unroll
+  for (int h = 0; h < 4; ++h)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float v = dpp_allreduce16(acc[h][r], [](float x, float y) { return x + y; });
+      got = c == 4 * h + r ? v : got;
+    }
+  if constexpr (C::WR > 1) {
+    s_sum[wave][lane] = got;
+    __syncthreads();
+    if (wr != 0) return;
+    got = 0.f;
+#pragma unroll
+    for (int w = 0; w < C::WR; ++w) got += s_sum[wk * C::WR + w][lane];
+  }
+  if (any && j < hi && my_page >= 0 && my_page < a.pages) {
+    float* w = a.weights + weight_at(a, my_page, head, j);
+    *w = (j < pos0 ? a.decay * *w : 0.f) + got;
+  }
+}
+
+}  // namespace
+}  // namespace lilicorr

@@ -1,9 +1,11 @@
-// The paged cache's bookkeeping and its writer: lilicorr_page_plan (places for one step's tokens) and
-// lilicorr_qk_norm_rope (head norms, rotation and cache write in one pass).
+// The paged cache's bookkeeping and its writers: lilicorr_page_plan (places for one step's tokens),
+// lilicorr_qk_norm_rope (head norms, rotation and cache write in one pass) and lilicorr_qk_norm_rope4 (the same into
+// a 4-bit cache).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
 
+#include "cache4.hpp"
 #include "common.hpp"
 #include "lilicorr.h"
 #include "paged.hpp"
@@ -229,8 +231,9 @@ struct RopeArgs {
   const float *q_weight, *k_weight;
   float eps;
   uint16_t *k_cache, *v_cache, *q_out;
-  int64_t pages, page_stride, token_stride, head_stride;
+  int64_t pages, page_stride, token_stride, head_stride;  // elements; bytes of codes with 4 bits
   int page_size;
+  unsigned char *k_scales, *v_scales;  // 4 bits
 };
 
 template <int LPH>
@@ -267,10 +270,11 @@ struct RopeLane {
   bool turned, upper;   // whether this lane's elements turn; whether they are the pairs' b
 };
 
-template <typename T, int LPH>
-__device__ __forceinline__ u32x4_t norm_turn(const u32x4_t& w, bool norm, const float (&wt)[8],
-                                             const float (&wp)[8], const RopeLane& r, int d,
-                                             float eps, int rot, int interleaved) {
+// y: the lane's eight elements; `size` (BOUND) for each the sum of the magnitudes that it was made from
+template <typename T, int LPH, bool BOUND>
+__device__ __forceinline__ void norm_turn32(const u32x4_t& w, bool norm, const float (&wt)[8],
+                                            const float (&wp)[8], const RopeLane& r, int d, float eps, int rot,
+                                            int interleaved, float (&y)[8], float (&size)[8]) {
   float x[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -286,15 +290,22 @@ __device__ __forceinline__ u32x4_t norm_turn(const u32x4_t& w, bool norm, const 
     s = head_sum<LPH>(s);
     inv = rsqrtf(s * (1.f / (float)d) + eps);
   }
-  float y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = norm ? x[i] * inv * wt[i] : x[i];
+  if constexpr (BOUND) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) size[i] = fabsf(y[i]);
+  }
   if (rot) {
     if (interleaved) {
       if (r.turned) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float a = y[2 * i], b = y[2 * i + 1];
+          if constexpr (BOUND) {
+            size[2 * i] = fabsf(a * r.cs[i]) + fabsf(b * r.sn[i]);
+            size[2 * i + 1] = fabsf(a * r.sn[i]) + fabsf(b * r.cs[i]);
+          }
           y[2 * i] = a * r.cs[i] - b * r.sn[i];
           y[2 * i + 1] = a * r.sn[i] + b * r.cs[i];
         }
@@ -310,6 +321,7 @@ __device__ __forceinline__ u32x4_t norm_turn(const u32x4_t& w, bool norm, const 
         for (int e = 0; e < 2; ++e) {
           const int j = 2 * i + e;
           const float z = norm ? t[e] * inv * wp[j] : t[e];
+          if constexpr (BOUND) size[j] = r.turned ? fabsf(y[j] * r.cs[j]) + fabsf(z * r.sn[j]) : size[j];
           // a c - b s for the lower half, b c + a s for the upper one
           const float turn = r.upper ? y[j] * r.cs[j] + z * r.sn[j] : y[j] * r.cs[j] - z * r.sn[j];
           y[j] = r.turned ? turn : y[j];
@@ -317,13 +329,174 @@ __device__ __forceinline__ u32x4_t norm_turn(const u32x4_t& w, bool norm, const 
       }
     }
   }
+}
+
+template <typename T, int LPH>
+__device__ __forceinline__ u32x4_t norm_turn(const u32x4_t& w, bool norm, const float (&wt)[8],
+                                             const float (&wp)[8], const RopeLane& r, int d,
+                                             float eps, int rot, int interleaved) {
+  float y[8], none[8];
+  norm_turn32<T, LPH, false>(w, norm, wt, wp, r, d, eps, rot, interleaved, y, none);
   u32x4_t out;
 #pragma unroll
   for (int i = 0; i < 4; ++i) out[i] = T::pack(y[2 * i], y[2 * i + 1]);
   return out;
 }
 
+// ---- the same in 4 bits ------------------------------------------------------------------------
+// A block of 32 elements lies in four neighbouring lanes. With the block's largest magnitude m 2^e, 1 <= m < 2, its
+// scale is 2^(e - 2) if m <= 7 / 4 and 2^(e - 1) if not; adding 2^21 - 1 to the mantissa's 23 bits carries into the
+// exponent in just the second case.
+__device__ __forceinline__ uint32_t scale4(float most) {
+  const int e = (int)((__float_as_uint(most) + 0x1fffffu) >> 23) - 2;  // of a biased exponent
+  return (uint32_t)min(max(e, (int)kLeastScale), (int)kMostScale);
+}
+
+// codes of eight elements: nearest, ties to the even code, saturating (the conversion's own rounding)
+__device__ __forceinline__ uint32_t codes4(const float (&y)[8], float scale) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
+  return w;
+}
+
+// the largest over four neighbouring lanes
+__device__ __forceinline__ float block_max(float v) {
+  v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, false)));
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, false)));
+}
+
+struct Code4 {
+  uint32_t w, scale;
+};
+
+// Values that are what they are: v as it comes.
+template <typename T>
+__device__ __forceinline__ Code4 quantise(const u32x4_t& w) {
+  float y[8], most = 0.f;
+  uint32_t bad = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = w[i];
+    const f32x2_t t = T::unpack(x);
+    y[2 * i] = t[0];
+    y[2 * i + 1] = t[1];
+    bad |= T::nonfinite(x);
+    most = fmaxf(most, fmaxf(fabsf(t[0]), fabsf(t[1])));
+  }
+  most = block_max(bad ? __builtin_inff() : most);
+  if (most == __builtin_inff()) return {0, kNanScale};
+  const uint32_t s = scale4(most);
+  return {codes4(y, scale_of(s)), s};
+}
+
+// A key in 64 bits, from its elements on: sums, norm, rotation, scale and codes. No contraction: each operation is
+// rounded as it stands in the formula.
 template <typename T, int LPH>
+__device__ __forceinline__ Code4 quantise64(const u32x4_t& w, bool norm, const float (&wt)[8], const float (&wp)[8],
+                                            const RopeLane& r, int d, float eps, int rot, int interleaved) {
+#pragma clang fp contract(off)
+  double x[8], s = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = w[i];
+    const f32x2_t t = T::unpack(u);
+    x[2 * i] = t[0];
+    x[2 * i + 1] = t[1];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s += x[i] * x[i];
+#pragma unroll
+  for (int m = 1; m < LPH; m <<= 1)
+    s += __longlong_as_double((long long)shfl_xor64((uint64_t)__double_as_longlong(s), m));
+  const double root = norm ? sqrt(s / d + (double)eps) : 1.0;
+  double y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = norm ? x[i] / root * (double)wt[i] : x[i];
+  if (rot && interleaved) {
+    if (r.turned) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const double a = y[2 * i], b = y[2 * i + 1], c = r.cs[i], n = r.sn[i];
+        y[2 * i] = a * c - b * n;
+        y[2 * i + 1] = a * n + b * c;
+      }
+    }
+  } else if (rot) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = (uint32_t)__shfl((int)w[i], r.partner, kWave);
+      const f32x2_t t = T::unpack(u);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int j = 2 * i + e;
+        const double z = norm ? (double)t[e] / root * (double)wp[j] : (double)t[e], c = r.cs[j], n = r.sn[j];
+        const double turn = r.upper ? z * n + y[j] * c : y[j] * c - z * n;
+        y[j] = r.turned ? turn : y[j];
+      }
+    }
+  }
+  double most = 0;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    bad |= !(fabs(y[i]) < __builtin_inf());
+    most = fmax(most, fabs(y[i]));
+  }
+  if (bad) most = __builtin_inf();
+#pragma unroll
+  for (int m = 1; m < 4; m <<= 1)
+    most = fmax(most, __longlong_as_double((long long)shfl_xor64((uint64_t)__double_as_longlong(most), m)));
+  if (most == __builtin_inf()) return {0, kNanScale};
+  int e;
+  const double f = frexp(most, &e);  // most = f 2^e, 0.5 <= f < 1
+  e = most == 0 ? -200 : e - (f <= 0.875 ? 3 : 2);
+  const int b = min(max(e + 127, (int)kLeastScale), (int)kMostScale);
+  const double back = ldexp(1.0, 127 - b);
+  uint32_t out = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const double v = fabs(y[i]) * back;  // exact
+    const uint32_t c = (v > 0.25) + (v >= 0.75) + (v > 1.25) + (v >= 1.75) + (v > 2.5) + (v >= 3.5) + (v > 5.0);
+    out |= (c | ((uint64_t)__double_as_longlong(y[i]) >> 63 ? 8u : 0u)) << (4 * i);
+  }
+  return {out, (uint32_t)b};
+}
+
+// A key: in fp32, and again in 64 bits by the whole wave where some element's scale, code or sign is not certain. An
+// element is at most 2^-20 of the magnitudes that it was made from off (sum of squares 13 roundings, halved by the
+// root; mean, root, two factors, two products and a sum: 16 in all of 2^-24), so it is certain where four times that
+// up or down changes nothing. With normal values one wave in 400 is done again.
+constexpr float kUncertain = 0x1p-18f;
+template <typename T, int LPH>
+__device__ __forceinline__ Code4 quantise_key(const u32x4_t& w, bool norm, const float (&wt)[8], const float (&wp)[8],
+                                              const RopeLane& r, int d, float eps, int rot, int interleaved) {
+  float y[8], size[8], lo[8], hi[8], most_lo = 0.f, most_hi = 0.f;
+  norm_turn32<T, LPH, true>(w, norm, wt, wp, r, d, eps, rot, interleaved, y, size);
+  bool unsure = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float off = size[i] * kUncertain, v = fabsf(y[i]);
+    lo[i] = v - off;
+    hi[i] = v + off;
+    unsure |= !(lo[i] > 0.f) && size[i] != 0.f;  // the sign; NaN
+    most_lo = fmaxf(most_lo, lo[i]);
+    most_hi = fmaxf(most_hi, hi[i]);
+  }
+  most_lo = block_max(most_lo);
+  most_hi = block_max(most_hi);
+  const uint32_t s = scale4(most_lo);
+  unsure |= !(most_hi < 0x1p126f) || s != scale4(most_hi);
+  const float scale = scale_of(s);
+  const uint32_t low = codes4(lo, scale);
+  unsure |= low != codes4(hi, scale);
+  if (__ballot(unsure)) return quantise64<T, LPH>(w, norm, wt, wp, r, d, eps, rot, interleaved);
+  return {codes4(y, scale), s};
+}
+
+template <typename T, int LPH, bool FOUR>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) {
   constexpr int kHeads = kWave / LPH;  // heads a wave holds
   const int lane = lane_id(), l = lane % LPH, g = lane / LPH;
@@ -409,6 +582,16 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
           if (!stored) break;
           const bool is_k = s + u < qs + ks;
           const int h = (is_k ? s + u - qs : s + u - qs - ks) * kHeads + g;
+          if constexpr (FOUR) {
+            const Code4 y = is_k ? quantise_key<T, LPH>(x[u], norm_k, kw, kp, r, a.d, a.eps, a.rot, a.interleaved)
+                                 : quantise<T>(x[u]);
+            const int64_t to = at + (int64_t)h * a.head_stride;
+            if (mine && h < a.kv_heads) {
+              *reinterpret_cast<uint32_t*>((unsigned char*)(is_k ? a.k_cache : a.v_cache) + to + l * 4) = y.w;
+              if (l % 4 == 0) (is_k ? a.k_scales : a.v_scales)[to / 16 + l / 4] = (unsigned char)y.scale;
+            }
+            continue;
+          }
           const u32x4_t y =
               is_k ? norm_turn<T, LPH>(x[u], norm_k, kw, kp, r, a.d, a.eps, a.rot, a.interleaved) : x[u];
           uint16_t* dst = (is_k ? a.k_cache : a.v_cache) + at + (int64_t)h * a.head_stride;
@@ -419,7 +602,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
   }
 }
 
-template <typename T>
+template <typename T, bool FOUR>
 void launch_rope(const RopeArgs& a, hipStream_t stream) {
   const int64_t items = a.tokens * a.parts, per = kRopeThreads / kWave;
   const int64_t want = (items + per - 1) / per;
@@ -427,11 +610,23 @@ void launch_rope(const RopeArgs& a, hipStream_t stream) {
   // workgroups, 86 to 88 with 2048 and more)
   const dim3 grid((unsigned)(want < 1024 ? want : 1024));
   if (a.d <= 64)
-    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 8>), grid, dim3(kRopeThreads), 0, stream, a);
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 8, FOUR>), grid, dim3(kRopeThreads), 0, stream, a);
   else if (a.d <= 128)
-    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 16>), grid, dim3(kRopeThreads), 0, stream, a);
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 16, FOUR>), grid, dim3(kRopeThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 32>), grid, dim3(kRopeThreads), 0, stream, a);
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, 32, FOUR>), grid, dim3(kRopeThreads), 0, stream, a);
+}
+
+// waves that share a token
+int rope_parts(int64_t tokens, int heads, int kv_heads, int d) {
+  // Few tokens: their steps spread over more waves, one each, or about three each while the waves have
+  // work at once anyway. With 12 steps a token (32 + 2 x 8 heads of 128): 16 tokens 3.6 us as 12 waves, 4.7
+  // as 4, 9.8 as 1; 256 tokens 5.5, 5.1, 10.3; 1024 tokens 12.9, 9.1, 11.8; 2048 tokens 13.3 as 4, 13.0 as
+  // 2, 14.6 as 1; 4096 tokens 22.0, 20.5, 20.1. The two limits were chosen there, for all widths.
+  const int each = d <= 64 ? 8 : d <= 128 ? 4 : 2;  // heads of a step
+  const int64_t steps = (heads + each - 1) / each + 2 * ((kv_heads + each - 1) / each);
+  const int64_t fit = 6144 / tokens, third = (steps + 2) / 3;
+  return (int)(tokens * steps <= 2400 ? steps : fit < 1 ? 1 : fit < third ? fit : third);
 }
 
 }  // namespace
@@ -518,7 +713,7 @@ extern "C" lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_arg
       rows_overlap(x.k, x.k_stride * 2, k_row, x.tokens, x.q_out, out_bytes) ||
       rows_overlap(x.v, x.v_stride * 2, k_row, x.tokens, x.q_out, out_bytes))
     return LILICORR_ERR_INVALID_ARG;
-  RopeArgs a;
+  RopeArgs a = {};
   a.q = (const uint16_t*)x.q; a.k = (const uint16_t*)x.k; a.v = (const uint16_t*)x.v;
   a.q_stride = x.q_stride; a.k_stride = x.k_stride; a.v_stride = x.v_stride;
   a.tokens = x.tokens;
@@ -531,15 +726,65 @@ extern "C" lilicorr_status lilicorr_qk_norm_rope(const lilicorr_qk_norm_rope_arg
   a.pages = c.pages; a.page_stride = c.page_stride; a.token_stride = c.token_stride;
   a.head_stride = c.head_stride;
   a.page_size = c.page_size;
-  // Few tokens: their steps spread over more waves, one each, or about three each while the waves have
-  // work at once anyway. With 12 steps a token (32 + 2 x 8 heads of 128): 16 tokens 3.6 us as 12 waves, 4.7
-  // as 4, 9.8 as 1; 256 tokens 5.5, 5.1, 10.3; 1024 tokens 12.9, 9.1, 11.8; 2048 tokens 13.3 as 4, 13.0 as
-  // 2, 14.6 as 1; 4096 tokens 22.0, 20.5, 20.1. The two limits were chosen there, for all widths.
-  const int each = c.d <= 64 ? 8 : c.d <= 128 ? 4 : 2;  // heads of a step
-  const int64_t steps = (x.heads + each - 1) / each + 2 * ((c.heads + each - 1) / each);
-  const int64_t fit = 6144 / x.tokens, third = (steps + 2) / 3;
-  a.parts = (int)(x.tokens * steps <= 2400 ? steps : fit < 1 ? 1 : fit < third ? fit : third);
-  if (c.dtype == LILICORR_BF16) launch_rope<Bf16>(a, stream);
-  else launch_rope<F16>(a, stream);
+  a.parts = rope_parts(x.tokens, x.heads, c.heads, c.d);
+  if (c.dtype == LILICORR_BF16) launch_rope<Bf16, false>(a, stream);
+  else launch_rope<F16, false>(a, stream);
+  return launch_status();
+}
+
+extern "C" lilicorr_status lilicorr_qk_norm_rope4(const lilicorr_qk_norm_rope4_args* args, hipStream_t stream) {
+  if (!args) return LILICORR_ERR_INVALID_ARG;
+  const lilicorr_qk_norm_rope4_args& x = *args;
+  const lilicorr_cache4& c = x.cache;
+  if (const lilicorr_status s = cache4_sizes(c)) return s;
+  if (x.dtype != LILICORR_BF16 && x.dtype != LILICORR_F16) return LILICORR_ERR_INVALID_ARG;
+  if (x.heads < 1 || x.tokens < 0 || x.rot < 0 || x.rot > c.d || x.max_positions < 0)
+    return LILICORR_ERR_INVALID_ARG;
+  if (!(x.eps >= 0.f) || !isfinite(x.eps)) return LILICORR_ERR_INVALID_ARG;
+  if (x.q_stride < 0 || x.k_stride < 0 || x.v_stride < 0) return LILICORR_ERR_INVALID_ARG;
+  if (x.rot % 16 || x.heads > 65535 || x.tokens > 0x7fffffffll) return LILICORR_ERR_UNSUPPORTED;
+  if (!stride_ok(x.q_stride) || !stride_ok(x.k_stride) || !stride_ok(x.v_stride))
+    return LILICORR_ERR_ALIGNMENT;
+  if (x.tokens == 0) return LILICORR_OK;
+  if (!x.q || !x.k || !x.v || !x.slots || !x.positions || !x.q_out || !c.k || !c.v || !c.k_scales || !c.v_scales ||
+      (x.rot > 0 && !x.cos_sin))
+    return LILICORR_ERR_INVALID_ARG;
+  // q rows that are turned in place must be laid out as the output is
+  if (x.q_out == x.q && x.tokens > 1 && x.q_stride != (int64_t)x.heads * c.d) return LILICORR_ERR_INVALID_ARG;
+  if (!aligned16(x.q) || !aligned16(x.k) || !aligned16(x.v) || !aligned16(x.q_out) || !aligned16(c.k) ||
+      !aligned16(c.v) || !aligned16(x.cos_sin) || !aligned16(x.q_weight) || !aligned16(x.k_weight) ||
+      !aligned4(x.slots) || !aligned4(x.positions))
+    return LILICORR_ERR_ALIGNMENT;
+  // what other waves still read must not lie where q_out does, nor q_out in the cache
+  const size_t q_row = (size_t)x.heads * c.d * 2, k_row = (size_t)c.heads * c.d * 2, out = q_row * (size_t)x.tokens;
+  const size_t span = cache4_span(c);
+  if ((x.q_out != x.q && rows_overlap(x.q, x.q_stride * 2, q_row, x.tokens, x.q_out, out)) ||
+      rows_overlap(x.k, x.k_stride * 2, k_row, x.tokens, x.q_out, out) ||
+      rows_overlap(x.v, x.v_stride * 2, k_row, x.tokens, x.q_out, out))
+    return LILICORR_ERR_INVALID_ARG;
+  const struct { const void* at; size_t bytes; } parts[] = {
+      {c.k, span}, {c.v, span}, {c.k_scales, cache4_scales(span)}, {c.v_scales, cache4_scales(span)}};
+  for (const auto& p : parts)
+    if (overlap(x.q_out, out, p.at, p.bytes) || rows_overlap(x.q, x.q_stride * 2, q_row, x.tokens, p.at, p.bytes) ||
+        rows_overlap(x.k, x.k_stride * 2, k_row, x.tokens, p.at, p.bytes) ||
+        rows_overlap(x.v, x.v_stride * 2, k_row, x.tokens, p.at, p.bytes))
+      return LILICORR_ERR_INVALID_ARG;
+  RopeArgs a = {};
+  a.q = (const uint16_t*)x.q; a.k = (const uint16_t*)x.k; a.v = (const uint16_t*)x.v;
+  a.q_stride = x.q_stride; a.k_stride = x.k_stride; a.v_stride = x.v_stride;
+  a.tokens = x.tokens;
+  a.heads = x.heads; a.kv_heads = c.heads; a.d = c.d; a.rot = x.rot;
+  a.interleaved = x.interleaved != 0;
+  a.slots = x.slots; a.positions = x.positions; a.cos_sin = x.cos_sin;
+  a.max_positions = x.max_positions;
+  a.q_weight = x.q_weight; a.k_weight = x.k_weight; a.eps = x.eps;
+  a.k_cache = (uint16_t*)c.k; a.v_cache = (uint16_t*)c.v; a.q_out = (uint16_t*)x.q_out;
+  a.k_scales = (unsigned char*)c.k_scales; a.v_scales = (unsigned char*)c.v_scales;
+  a.pages = c.pages; a.page_stride = c.page_stride; a.token_stride = c.token_stride;
+  a.head_stride = c.head_stride;
+  a.page_size = c.page_size;
+  a.parts = rope_parts(x.tokens, x.heads, c.heads, c.d);
+  if (x.dtype == LILICORR_BF16) launch_rope<Bf16, true>(a, stream);
+  else launch_rope<F16, true>(a, stream);
   return launch_status();
 }
