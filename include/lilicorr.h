@@ -639,7 +639,7 @@ lilicorr_status lilicorr_prefix_attention(const lilicorr_attention_args *args, h
  */
 typedef struct {
     void *k, *v;              /* codes, 16-byte aligned */
-    void *k_scales, *v_scales; /* bytes */
+    void *k_scales, *v_scales; /* bytes, 4-byte aligned */
     int page_size;
     int heads;                /* key heads */
     int d;                    /* head width: a multiple of 32, at most 256 */

@@ -11,6 +11,12 @@
 
 namespace lilicorr {
 namespace {
+#ifndef LEAST_TILES
+#define LEAST_TILES 65536
+#endif
+#ifndef CHUNK_TILES
+#define CHUNK_TILES 64
+#endif
 
 constexpr size_t kLeastBytes4 = 256;  // of a workspace
 // The longest sequences have so many tokens: lengths, windows and sinks past it say "without end"
@@ -19,40 +25,48 @@ int64_t bounded4(int64_t n) { return n < kMost4 ? n : kMost4; }
 
 struct Plan4 {
   int BM, tiles, chunk, chunks;  // rows of a tile; row tiles; 32-key tiles of a chunk; chunks
-  bool fast, spread;
+  int heads;  // key heads that a workgroup's waves share
+  bool ring, spread;
   int64_t rows;
   size_t bytes;  // of the workspace
 };
 
-// Calls `use` with the kernel of a width and tile height. Up to 64 rows the waves share the keys, and a wave has all the
-// rows as long as they fit its registers; wider heads, and the two terms of fp16, leave room for fewer.
-template <typename T, int D, bool FAST, typename F>
-void with_rows4(int BM, const F& use) {
-  if (BM == 16) return use(Attn4Config<T, D, 1, 1, 4, FAST>());
-  if constexpr (D > 128) {
-    if (BM == 32) return use(Attn4Config<T, D, 1, 2, 2, FAST>());
-    return use(Attn4Config<T, D, 1, 4, 1, FAST>());
-  } else {
-    if (BM == 32) return use(Attn4Config<T, D, 2, 1, 4, FAST>());
-    if constexpr (D <= 64 || Query<T>::kTerms == 1) {
-      if (BM == 64) return use(Attn4Config<T, D, 4, 1, 4, FAST>());
-    } else {
-      if (BM == 64) return use(Attn4Config<T, D, 2, 2, 2, FAST>());
+// Calls `use` with the kernel of a width, a tile height and what the workgroup's waves share: key heads (`heads`: a token's
+// heads lie side by side, and so share cache lines) or keys.
+template <typename T, int D, bool RING, typename F>
+void with_rows4(int BM, bool heads, const F& use) {
+  if constexpr (RING) {
+    if (heads) {
+      if (BM == 16) return use(Attn4Config<T, D, 1, 4, 1, 1, RING>());
+      if constexpr (D <= 128) {
+        if (BM == 32) return use(Attn4Config<T, D, 2, 4, 1, 1, RING>());
+        if (BM == 64) return use(Attn4Config<T, D, 2, 2, 2, 1, RING>());
+      } else {
+        if (BM == 32) return use(Attn4Config<T, D, 1, 2, 2, 1, RING>());
+      }
     }
-    return use(Attn4Config<T, D, 2, 4, 1, FAST>());
+  }
+  if (BM == 16) return use(Attn4Config<T, D, 1, 1, 1, 4, RING>());
+  if constexpr (D > 128) {
+    if (BM == 32) return use(Attn4Config<T, D, 1, 1, 2, 2, RING>());
+    return use(Attn4Config<T, D, 1, 1, 4, 1, RING>());
+  } else {
+    if (BM == 32) return use(Attn4Config<T, D, 2, 1, 1, 4, RING>());
+    if (BM == 64) return use(Attn4Config<T, D, 2, 1, 2, 2, RING>());
+    return use(Attn4Config<T, D, 2, 1, 4, 1, RING>());
   }
 }
 int tile_rows4(int64_t rows, int d) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || d > 128 ? 64 : 128; }
 
 template <typename T, typename F>
-void with_kernel4(int d, bool fast, int BM, const F& use) {
+void with_kernel4(int d, bool ring, int BM, bool heads, const F& use) {
   auto width = [&](auto f) {
-    constexpr bool FAST = decltype(f)::value;
-    if (d <= 64) with_rows4<T, 64, FAST>(BM, use);
-    else if (d <= 128) with_rows4<T, 128, FAST>(BM, use);
-    else with_rows4<T, 256, FAST>(BM, use);
+    constexpr bool RING = decltype(f)::value;
+    if (d <= 64) with_rows4<T, 64, RING>(BM, heads, use);
+    else if (d <= 128) with_rows4<T, 128, RING>(BM, heads, use);
+    else with_rows4<T, 256, RING>(BM, heads, use);
   };
-  if (fast) width(std::true_type());
+  if (ring) width(std::true_type());
   else width(std::false_type());
 }
 
@@ -72,6 +86,15 @@ lilicorr_status sizes4(const A& a) {
   // 16 keys of a page are reached with 32-bit offsets
   if (a.cache.token_stride >= (int64_t)1 << 27) return LILICORR_ERR_UNSUPPORTED;
   return LILICORR_OK;
+}
+
+// whether tiles can go by way of LDS: 16 keys in a page, whole rows of 64, 128 or 256, scales where the copies' 4 bytes (2
+// with heads of 64) want them
+bool ring_fits(const lilicorr_cache4& c) {
+  if (c.page_size % 16 || (c.d != 64 && c.d != 128 && c.d != 256)) return false;
+  const int64_t unit = c.d == 64 ? 2 : 4;
+  auto even = [&](int64_t s) { return s % (16 * unit) == 0; };
+  return even(c.page_stride) && even(c.token_stride) && even(c.head_stride);
 }
 
 lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
@@ -95,16 +118,26 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
     if (tiles32 < most) most = tiles32;
   }
   if (most < 1) most = 1;
-  p.fast = a.cache.page_size % 16 == 0;
+  p.ring = ring_fits(a.cache);
   p.spread = own <= p.BM;
-  // chunks so that all compute units have work
-  const int64_t items = tiles * a.cache.heads, wk = p.BM <= 64 ? 4 : 1;
-  const int64_t want = 768;
-  int64_t chunks = items >= want ? 1 : want / items;
-  const int64_t fit = (most + 2 * wk - 1) / (2 * wk);
-  if (chunks > fit) chunks = fit;
-  if (chunks > 64) chunks = 64;
-  const int64_t chunk = (most + chunks - 1) / chunks;
+  // key heads over the waves, where that still leaves every compute unit work
+  const int wide = p.BM <= 16 || (p.BM == 32 && a.cache.d <= 128) ? 4 : p.BM <= 64 && (a.cache.d <= 128 || p.BM == 32) ? 2 : 1;
+  const int64_t pairs = tiles * a.cache.heads;
+  p.heads = p.ring && wide > 1 && a.cache.heads % wide == 0 && pairs * most >= LEAST_TILES ? wide : 1;
+  const int64_t items = pairs / p.heads, wk = p.heads > 1 ? 1 : p.BM <= 32 ? (p.BM == 32 && a.cache.d > 128 ? 2 : 4) : p.BM == 64 && a.cache.d <= 128 ? 2 : 1;
+  int64_t chunk, chunks;
+  if (p.heads > 1) {
+    chunk = CHUNK_TILES;
+    chunks = (most + chunk - 1) / chunk;
+    if (chunks > 64) chunks = 64;
+  } else {
+    const int64_t want = 768;
+    chunks = items >= want ? 1 : want / items;
+    const int64_t fit = (most + 2 * wk - 1) / (2 * wk);
+    if (chunks > fit) chunks = fit;
+    if (chunks > 64) chunks = 64;
+  }
+  chunk = (most + chunks - 1) / chunks;
   chunks = (most + chunk - 1) / chunk;
   if (tiles * chunks > 0x7fffffffll / a.cache.heads) return LILICORR_ERR_UNSUPPORTED;
   p.tiles = (int)tiles;
@@ -138,13 +171,16 @@ Attn4Args common4(const A& x) {
 
 template <typename C>
 void launch4(const Attn4Args& a, hipStream_t stream) {
-  if constexpr (C::kLds > 65536) {
+  constexpr uint32_t kRing = C::RING ? C::kWaves * Ring4<C, true>::kBytes : 0;
+  constexpr uint32_t kLds = kRing > C::kJoin ? kRing : C::kJoin;
+  static_assert(kLds <= 160 * 1024, "a workgroup fits");
+  if constexpr (kLds > 65536) {
     static const hipError_t attr =
         hipFuncSetAttribute(reinterpret_cast<const void*>(attention4_kernel<C>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::kLds);
+                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
     (void)attr;
   }
-  hipLaunchKernelGGL(attention4_kernel<C>, dim3((unsigned)a.items), dim3(C::kThreads), C::kLds, stream, a);
+  hipLaunchKernelGGL(attention4_kernel<C>, dim3((unsigned)a.items), dim3(C::kThreads), kLds, stream, a);
 }
 
 template <typename T, int LPR>
@@ -162,12 +198,12 @@ lilicorr_status run4(const lilicorr_attention4_args& x, const Plan4& p, hipStrea
   a.window = (int)bounded4(x.window);
   a.sinks = (int)bounded4(x.sinks);
   a.tiles = p.tiles; a.chunk = p.chunk; a.most = p.chunk * p.chunks;
-  a.items = p.tiles * p.chunks * a.kv_heads;
+  a.items = p.tiles * p.chunks * (a.kv_heads / p.heads);
   a.spread = p.spread;
   a.split = p.chunks > 1;
   a.part_o = (float*)x.workspace;
   a.part_ml = (f32x4_t*)((unsigned char*)x.workspace + (size_t)p.chunks * p.rows * a.d * 4);
-  with_kernel4<T>(a.d, p.fast, p.BM, [&](auto c) { launch4<decltype(c)>(a, stream); });
+  with_kernel4<T>(a.d, p.ring, p.BM, p.heads > 1, [&](auto c) { launch4<decltype(c)>(a, stream); });
   if (a.split) {
     if (a.d <= 64) launch_join4<T, 16>(a, p.chunks, stream);
     else if (a.d <= 128) launch_join4<T, 32>(a, p.chunks, stream);
@@ -177,7 +213,7 @@ lilicorr_status run4(const lilicorr_attention4_args& x, const Plan4& p, hipStrea
 }
 
 // keys of a tile of key_weights_many_kernel: WK waves of 64
-template <typename T, bool FAST>
+template <typename T, bool RING>
 void launch_weights(Attn4Args a, int d, hipStream_t stream) {
   const bool few = (int64_t)a.max_tokens * a.group <= 16;
   int64_t keys = (int64_t)a.table_width * a.page_size;
@@ -186,27 +222,36 @@ void launch_weights(Attn4Args a, int d, hipStream_t stream) {
   auto run = [&](auto width) {
     constexpr int D = decltype(width)::value;
     if (few) {
-      typedef Attn4Config<T, D, 1, 1, 4, FAST> C;
-      const int64_t most = (keys + 31) / 32, items = (int64_t)a.N * a.kv_heads, want = 1024;
-      int64_t chunks = items >= want ? 1 : want / items;
-      const int64_t fit = (most + 7) / 8;
+      const int64_t most = (keys + 31) / 32;
+      auto launch = [&](auto c, int64_t items, int64_t chunk) {
+        typedef decltype(c) C;
+        a.tiles = a.N;
+        a.chunk = (int)chunk;
+        a.items = (int)(items * ((most + chunk - 1) / chunk));
+        a.spread = 1;
+        constexpr uint32_t kLds = C::RING ? C::kWaves * Ring4<C, false>::kBytes : 0;
+        static_assert(kLds <= 65536, "no attribute is asked for");
+        hipLaunchKernelGGL(key_weights_few_kernel<C>, dim3((unsigned)a.items), dim3(C::kThreads), kLds, stream, a);
+      };
+      const int64_t pairs = (int64_t)a.N * a.kv_heads;
+      if constexpr (RING) {
+        if (a.kv_heads % 4 == 0 && pairs * most >= LEAST_TILES)
+          return launch(Attn4Config<T, D, 1, 4, 1, 1, RING>(), pairs / 4, CHUNK_TILES);
+      }
+      const int64_t want = 1024, fit = (most + 7) / 8;
+      int64_t chunks = pairs >= want ? 1 : want / pairs;
       if (chunks > fit) chunks = fit;
-      a.tiles = a.N;
-      a.chunk = (int)((most + chunks - 1) / chunks);
-      chunks = (most + a.chunk - 1) / a.chunk;
-      a.items = (int)(items * chunks);
-      a.spread = 1;
-      hipLaunchKernelGGL(key_weights_few_kernel<C>, dim3((unsigned)a.items), dim3(C::kThreads), 0, stream, a);
+      launch(Attn4Config<T, D, 1, 1, 1, 4, RING>(), pairs, (most + chunks - 1) / chunks);
     } else {
       const int64_t groups = (keys + 63) / 64;
       // enough key groups: neighbouring ones share the rows that they read; else the waves share the rows
       if (groups * a.N * a.kv_heads >= 2048) {
-        typedef Attn4Config<T, D, 1, 1, 4, FAST> C;
+        typedef Attn4Config<T, D, 1, 1, 1, 4, false> C;
         a.tiles = (int)((groups + 3) / 4);
         hipLaunchKernelGGL(key_weights_many_kernel<C>, dim3((unsigned)((int64_t)a.tiles * a.N * a.kv_heads)),
                            dim3(C::kThreads), 0, stream, a);
       } else {
-        typedef Attn4Config<T, D, 1, 4, 1, FAST> C;
+        typedef Attn4Config<T, D, 1, 1, 4, 1, false> C;
         a.tiles = (int)groups;
         hipLaunchKernelGGL(key_weights_many_kernel<C>, dim3((unsigned)((int64_t)a.tiles * a.N * a.kv_heads)),
                            dim3(C::kThreads), 0, stream, a);
@@ -224,7 +269,7 @@ lilicorr_status run_weights(const lilicorr_key_weights_args& x, hipStream_t stre
   a.lse_in = x.lse;
   a.weights = x.weights;
   a.decay = x.decay;
-  if (x.cache.page_size % 16 == 0) launch_weights<T, true>(a, a.d, stream);
+  if (ring_fits(x.cache)) launch_weights<T, true>(a, a.d, stream);
   else launch_weights<T, false>(a, a.d, stream);
   return launch_status();
 }
@@ -249,7 +294,7 @@ extern "C" lilicorr_status lilicorr_window_attention4(const lilicorr_attention4_
   if (!x.q || !x.out || !c.k || !c.v || !c.k_scales || !c.v_scales || !x.table || !x.starts || !x.totals || x.q == x.out)
     return LILICORR_ERR_INVALID_ARG;
   if (!aligned16(x.q) || !aligned16(x.out) || !aligned16(c.k) || !aligned16(c.v) || !aligned16(x.workspace) ||
-      !aligned4(x.lse) || !aligned4(x.table) || !aligned4(x.starts) || !aligned4(x.totals))
+      !aligned4(x.lse) || !aligned4(c.k_scales) || !aligned4(c.v_scales) || !aligned4(x.table) || !aligned4(x.starts) || !aligned4(x.totals))
     return LILICORR_ERR_ALIGNMENT;
   if (!x.workspace || x.workspace_bytes < p.bytes) return LILICORR_ERR_WORKSPACE;
   if (x.max_tokens == 0) return LILICORR_OK;
@@ -272,7 +317,7 @@ extern "C" lilicorr_status lilicorr_key_weights(const lilicorr_key_weights_args*
   if (x.tokens == 0) return LILICORR_OK;
   if (!x.q || !x.lse || !x.weights || !c.k || !c.k_scales || !x.table || !x.starts || !x.totals)
     return LILICORR_ERR_INVALID_ARG;
-  if (!aligned16(x.q) || !aligned16(c.k) || !aligned16(x.weights) || !aligned4(x.lse) || !aligned4(x.table) ||
+  if (!aligned16(x.q) || !aligned16(c.k) || !aligned16(x.weights) || !aligned4(x.lse) || !aligned4(c.k_scales) || !aligned4(x.table) ||
       !aligned4(x.starts) || !aligned4(x.totals))
     return LILICORR_ERR_ALIGNMENT;
   if (x.max_tokens == 0) return LILICORR_OK;

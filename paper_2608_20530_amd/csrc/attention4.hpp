@@ -71,14 +71,15 @@ struct Attn4Args {
   float decay;
 };
 
-template <typename T_, int D_, int RT_, int WR_, int WK_, bool FAST_>
+template <typename T_, int D_, int RT_, int WH_, int WR_, int WK_, bool RING_>
 struct Attn4Config {
   typedef T_ T;
   static constexpr int D = D_;    // heads of D elements or fewer
   static constexpr int RT = RT_;  // blocks of 16 rows of a wave
-  static constexpr int WR = WR_, WK = WK_;  // waves of rows by waves of keys
-  static constexpr bool FAST = FAST_;  // pages of a multiple of 16 tokens: 16 keys in one place
-  static constexpr int kWaves = WR * WK, kThreads = kWaves * kWave;
+  static constexpr int WH = WH_, WR = WR_, WK = WK_;  // waves of key heads by waves of rows by waves of keys
+  static constexpr bool RING = RING_;  // tiles by way of LDS
+  static constexpr int NS = D <= 64 ? 4 : D <= 128 ? 3 : 2;  // stages of a wave's ring
+  static constexpr int kWaves = WH * WR * WK, kThreads = kWaves * kWave;
   static constexpr int BM = 16 * RT * WR;
   static constexpr int ND = D / 16;  // output products
   static constexpr int KW = D / 32;  // 32-bit words that a lane has of a key
@@ -87,7 +88,11 @@ struct Attn4Config {
   static constexpr int kTerms = Query<T>::kTerms;
   // the waves' partial outputs, in the order of their lanes, and sums
   static constexpr uint32_t kOut = kWaves * RT * ND * kWave * 16, kSums = kWaves * RT * kWave * 16;
-  static constexpr uint32_t kLds = WK > 1 ? kOut + kSums : 0;
+  static constexpr uint32_t kJoin = WK > 1 ? kOut + kSums : 0;
+  // waves of a SIMD that the registers are given out for: two or more keep the accumulators where the vector unit
+  // reaches them
+  static constexpr int kSimdWaves =
+      D > 128 || RT == 4 || (RT == 2 && D > 64 && kTerms > 1) ? 1 : RT == 1 && kTerms == 1 ? 3 : 2;
 };
 
 // What a wave has under way of a tile of 32 keys
@@ -101,14 +106,12 @@ __device__ __forceinline__ int entry4(const Attn4Args& a, int j) {
   return (int)(((uint64_t)(uint32_t)j * a.page_mul) >> a.page_shift);
 }
 
-// Where a wave's lanes find a tile's keys. `page` (one register) is the page of key lane % 32 of the tile, asked for
-// a tile ahead. FAST: two uniform bases, and offsets that a lane keeps; otherwise each key's own.
+// What a lane has of a key and a value, where loads go straight to registers
 template <typename C>
 struct Places4 {
-  uint32_t k_lane, v_lane;    // bytes of a lane's part within a key's, a value's codes
+  uint32_t k_lane, v_lane;              // bytes of the lane's part within a key's, a value's codes
   uint32_t k_scale, k_scale2, v_scale;  // and within its scales
-  uint32_t k_off, v_off;      // FAST: the same with the lane's (first) key
-  uint32_t ks_off, vs_off;
+  uint32_t k_more;                      // from there to the second 16 bytes of a wide head's key
 
   __device__ __forceinline__ void set(const Attn4Args& a) {
     const int lane = lane_id(), c = lane & 15, g = lane >> 4;
@@ -116,14 +119,10 @@ struct Places4 {
     const int ke = g * (C::D / 4), ve = c * (C::D / 16);
     k_lane = ke < a.d ? ke / 2 : 0;
     k_scale = ke < a.d ? ke / kBlock4 : 0;
-    k_scale2 = ke + kBlock4 < a.d ? ke / kBlock4 + 1 : 0;
+    k_more = C::D > 128 && ke + kBlock4 < a.d ? 16 : 0;
+    k_scale2 = k_scale + k_more / 16;
     v_lane = ve < a.d ? ve / 2 : 0;
     v_scale = ve < a.d ? ve / kBlock4 : 0;
-    const uint32_t ts = (uint32_t)a.token_stride;
-    k_off = c * ts + k_lane;
-    v_off = 4 * g * ts + v_lane;
-    ks_off = c * (ts / 16) + k_scale;
-    vs_off = 4 * g * (ts / 16) + v_scale;
   }
 };
 
@@ -139,77 +138,259 @@ __device__ __forceinline__ void load_bytes(const unsigned char* p, uint32_t* to)
     to[1] = w[1];
   } else {
     const u32x4_t w = *reinterpret_cast<const u32x4_t*>(p);
-    to[0] = w[0];
-    to[1] = w[1];
-    to[2] = w[2];
-    to[3] = w[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[i] = w[i];
   }
 }
 
-// a lane's part of a key; the second half of a wide one lies 16 bytes on, or is the head's first where that ends
-template <typename C>
-__device__ __forceinline__ void load_key(const unsigned char* at, bool more, uint32_t* to) {
-  if constexpr (C::D <= 128) {
-    load_bytes<C::D / 8>(at, to);
-  } else {
-    load_bytes<16>(at, to);
-    load_bytes<16>(more ? at + 16 : at, to + 4);
-  }
-}
-
-// asks for the keys (and with VALUES the values) of a tile of 32
+// Asks for the keys (and with VALUES the values) of a tile of 32, any pages and widths. `page` (one register) is the page
+// of key lane % 32. The second half of a wide head's part of a key lies 16 bytes on, or is its first where the head
+// ends.
 template <typename C, bool VALUES>
 __device__ __forceinline__ void load4(const Attn4Args& a, const Places4<C>& pl, const unsigned char* k,
                                       const unsigned char* v, const unsigned char* ks, const unsigned char* vs,
                                       int tile, int page, Raw4<C>& r) {
   const int lane = lane_id(), c = lane & 15, g = lane >> 4;
-  const bool more = g * (C::D / 4) + kBlock4 < a.d;
-  if constexpr (C::FAST) {
+  const int j = tile * 32 + (lane & 31);
+  const uint64_t mine = (uint64_t)(uint32_t)page * (uint64_t)a.page_stride +
+                        (uint64_t)((uint32_t)j - (uint32_t)entry4(a, j) * a.page_size) * (uint64_t)a.token_stride;
+  const uint32_t lo = (uint32_t)(mine >> 4), hi = (uint32_t)(mine >> 36);  // in 16 bytes
+  auto of = [&](int key) {
+    const uint32_t x = (uint32_t)__builtin_amdgcn_ds_bpermute(key * 4, (int)lo);
+    const uint32_t y = (uint32_t)__builtin_amdgcn_ds_bpermute(key * 4, (int)hi);
+    return (uint64_t)y << 32 | x;
+  };
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int j = tile * 32 + h * 16;
-      const int p = (int)readlane32((uint32_t)page, h * 16);
-      const uint64_t base = (uint64_t)p * (uint64_t)a.page_stride +
-                            (uint64_t)((uint32_t)j - (uint32_t)entry4(a, j) * a.page_size) * (uint64_t)a.token_stride;
-      const unsigned char *kb = k + base, *vb = v + base, *kt = ks + base / 16, *vt = vs + base / 16;
-      load_key<C>(kb + pl.k_off, more, r.k[h]);
-      r.ks[h][0] = kt[pl.ks_off];
-      if constexpr (C::KS > 1) r.ks[h][1] = kt[pl.ks_off - pl.k_scale + pl.k_scale2];
-      if constexpr (VALUES) {
+  for (int h = 0; h < 2; ++h) {
+    const uint64_t at = of(16 * h + c);
+    load_bytes<C::D <= 128 ? C::D / 8 : 16>(k + (at << 4) + pl.k_lane, r.k[h]);
+    if constexpr (C::D > 128) load_bytes<16>(k + (at << 4) + pl.k_lane + pl.k_more, r.k[h] + 4);
+    r.ks[h][0] = ks[at + pl.k_scale];
+    if constexpr (C::KS > 1) r.ks[h][1] = ks[at + pl.k_scale2];
+    if constexpr (VALUES) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          load_bytes<C::VB>(vb + e * a.token_stride + pl.v_off, r.v[4 * h + e]);
-          r.vs[4 * h + e] = (vt + e * (a.token_stride / 16))[pl.vs_off];
-        }
-      }
-    }
-  } else {
-    const int j = tile * 32 + (lane & 31);
-    const uint64_t mine = (uint64_t)(uint32_t)page * (uint64_t)a.page_stride +
-                          (uint64_t)((uint32_t)j - (uint32_t)entry4(a, j) * a.page_size) * (uint64_t)a.token_stride;
-    const uint32_t lo = (uint32_t)(mine >> 4), hi = (uint32_t)(mine >> 36);  // in 16 bytes
-    auto of = [&](int key) {
-      const uint32_t x = (uint32_t)__builtin_amdgcn_ds_bpermute(key * 4, (int)lo);
-      const uint32_t y = (uint32_t)__builtin_amdgcn_ds_bpermute(key * 4, (int)hi);
-      return (uint64_t)y << 32 | x;
-    };
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint64_t at = of(16 * h + c);
-      load_key<C>(k + (at << 4) + pl.k_lane, more, r.k[h]);
-      r.ks[h][0] = ks[at + pl.k_scale];
-      if constexpr (C::KS > 1) r.ks[h][1] = ks[at + pl.k_scale2];
-      if constexpr (VALUES) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint64_t to = of(16 * h + 4 * g + e);
-          load_bytes<C::VB>(v + (to << 4) + pl.v_lane, r.v[4 * h + e]);
-          r.vs[4 * h + e] = vs[to + pl.v_scale];
-        }
+      for (int e = 0; e < 4; ++e) {
+        const uint64_t to = of(16 * h + 4 * g + e);
+        load_bytes<C::VB>(v + (to << 4) + pl.v_lane, r.v[4 * h + e]);
+        r.vs[4 * h + e] = vs[to + pl.v_scale];
       }
     }
   }
 }
+
+// ---- the ring ------------------------------------------------------------------------------------
+// The rule (pages of a multiple of 16 tokens, heads of 64, 128 or 256): a wave copies its tiles to LDS, 16 bytes a lane
+// and neighbouring lanes neighbouring bytes, NS of them in turn. Loads straight to registers in the operands' layout take four
+// times as long: a load instruction costs the address unit 16 steps and more however little it brings, and lanes
+// that are neighbours there have different keys (counted: 336 cache accesses a tile; 256 requests of one token 603 us).
+// 16 keys lie in one page, so a copy has a uniform base; pieces of 16 bytes are permuted, and values' rows too, so that
+// the operands' reads meet no bank conflicts.
+typedef __attribute__((address_space(3))) unsigned char* lds_t;
+typedef __attribute__((address_space(3))) uint32_t* lds_u32_t;
+typedef __attribute__((address_space(3))) float* lds_float_t;
+typedef __attribute__((address_space(3))) u32x4_t* lds_u32x4_t;
+
+// Copies to LDS at `dst` in lane order, counted by vmcnt alone; no register is loaded, so none is in flight. WIDE: 16
+// bytes a lane from a uniform base and the lane's offset. Else 4 bytes, or with SHORT 2 in 4, from the lane's address.
+__device__ __forceinline__ void copy16(lds_t dst, const unsigned char* base, uint32_t lane) {
+  const uint32_t at = uniform32((uint32_t)(uintptr_t)dst);
+  __asm__ volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(at), "v"(lane), "s"(base) : "memory");
+}
+__device__ __forceinline__ void copy16(lds_t dst, const unsigned char* from) {
+  const uint32_t at = uniform32((uint32_t)(uintptr_t)dst);
+  __asm__ volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(at), "v"(from) : "memory");
+}
+template <bool SHORT>
+__device__ __forceinline__ void copy4(lds_t dst, const unsigned char* from) {
+  const uint32_t at = uniform32((uint32_t)(uintptr_t)dst);
+  if constexpr (SHORT)
+    __asm__ volatile("s_nop 0\n\tglobal_load_lds_ushort %1, off" ::"{m0}"(at), "v"(from) : "memory");
+  else
+    __asm__ volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(at), "v"(from) : "memory");
+}
+
+// (by value: a choice between two members would put the structure into memory)
+template <typename X>
+__device__ __forceinline__ X pick(bool first, X a, X b) {
+  return first ? a : b;
+}
+
+template <typename C, bool VALUES>
+struct Ring4 {
+  static constexpr int D = C::D, RB = D / 2;      // bytes of a key's codes
+  static constexpr int CPR = D / 32;              // 16-byte pieces of them
+  static constexpr int KI = 32 * CPR / kWave;     // copies of a tile's keys, D = 64, 128, 256: 1, 2, 4
+  static constexpr int SB = D <= 128 ? 4 : 8;     // bytes of a key's scales, in LDS
+  static constexpr uint32_t kV = 32 * RB, kS = VALUES ? 2 * kV : kV;
+  static constexpr uint32_t kW = kS + 256;  // without values: the keys' weights
+  static constexpr uint32_t kStage = kS + (D <= 128 && VALUES ? 256 : 512);
+  static constexpr int IPS = KI * (VALUES ? 2 : 1) + (D <= 128 && VALUES ? 1 : 2);  // copies of a stage
+  static constexpr int NS = C::NS;
+  static constexpr int kEntries = 128;            // of the page table, which the wave keeps
+  static constexpr uint32_t kBytes = NS * kStage + kEntries * 4;
+
+  const unsigned char *k, *v, *ks, *vs;
+  const int32_t* trow;
+  lds_t lds;
+  uint32_t k_off[2], v_off[2];  // of a lane's piece: bytes
+  uint32_t s_off;
+  uint32_t k_at, k_x, v_at, ks_at, vs_at;  // LDS offsets of its reads
+  int x0, e_last;               // first entry that is kept, last one that there is
+  bool absent;                  // a page among those so far is not there
+
+  __device__ __forceinline__ void set(const Attn4Args& a, const unsigned char* k_, const unsigned char* v_,
+                                      const unsigned char* ks_, const unsigned char* vs_, const int32_t* trow_,
+                                      int keys, lds_t lds_) {
+    k = k_; v = v_; ks = ks_; vs = vs_; trow = trow_; lds = lds_;
+    const int lane = lane_id(), c = lane & 15, g = lane >> 4;
+    const uint32_t ts = (uint32_t)a.token_stride;
+    // LDS row r of a half has key r, piece x at place x ^ swizzle(r), or of values key 4 (r % 4) + r / 4 as it is
+    const int per = D == 64 ? 32 : kWave;  // lanes that a half's (or with 256 a quarter's) rows take
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int r = (lane % per) / CPR + (D == 256 ? 8 * y : 0), x = lane % CPR;
+      k_off[y] = r * ts + (x ^ swizzle(r)) * 16;
+      v_off[y] = (4 * (r % 4) + r / 4) * ts + x * 16;
+    }
+    s_off = (D <= 128 ? lane % 16 : lane / 2 % 16) * (ts / 16) + (D <= 128 ? 0 : lane % 2 * 4);
+    k_at = c * RB + (D == 64 ? (uint32_t)((g / 2 ^ swizzle(c)) * 16 + g % 2 * 8) : 0u);
+    k_x = swizzle(c);
+    v_at = kV + g * RB + c * C::VB;
+    ks_at = kS + c * SB + (D == 64 ? g / 2 : D == 128 ? g : 2 * g);
+    vs_at = kS + 32 * SB + 4 * g * SB + (D > 128 ? c / 2 : 0);
+    x0 = -kEntries;
+    absent = false;
+    e_last = entry4(a, keys - 1);
+  }
+  static __device__ __forceinline__ uint32_t swizzle(int r) {
+    return D == 64 ? (r >> 3) & 1 : D == 128 ? (r >> 2) & 3 : (r >> 1) & 7;
+  }
+
+  // offsets (bytes of codes) of the two halves of the tile of 32 keys from `tile`'s first on
+  struct At {
+    uint64_t off0, off1;
+    int64_t w0, w1;      // of the first key's weight, without values
+    bool there0, there1; // whether the page is there
+  };
+  __device__ __forceinline__ At find(const Attn4Args& a, int tile, int head = 0) {
+    const int e0 = min(entry4(a, tile * 32), e_last), e1 = min(entry4(a, tile * 32 + 16), e_last);
+    const lds_u32_t kept = (lds_u32_t)(lds + NS * kStage);
+    if (e0 < x0 || e1 >= x0 + kEntries) {  // (uniform)
+      x0 = e0;
+      uint32_t page[kEntries / kWave];
+      bool gone = false;
+#pragma unroll
+      for (int u = 0; u < kEntries / kWave; ++u) page[u] = (uint32_t)trow[min(x0 + u * kWave + lane_id(), e_last)];
+#pragma unroll
+      for (int u = 0; u < kEntries / kWave; ++u) {
+        gone |= page[u] >= (uint32_t)a.pages;
+        kept[u * kWave + lane_id()] = page[u];
+      }
+      absent |= __ballot(gone) != 0;
+    }
+    const uint32_t pages = kept[(lane_id() < 32 ? e0 : e1) - x0];
+    At r;
+    auto half = [&](int h, uint64_t& off, int64_t& w, bool& there) __attribute__((always_inline)) {
+      const int j = tile * 32 + 16 * h;
+      uint32_t page = readlane32(pages, 32 * h);
+      there = page < (uint32_t)a.pages;
+      page = there ? page : 0;
+      const uint32_t o = (uint32_t)j - (uint32_t)entry4(a, j) * a.page_size;
+      off = (uint64_t)page * (uint64_t)a.page_stride + (uint64_t)o * (uint64_t)a.token_stride;
+      w = VALUES ? 0 : ((int64_t)page * a.kv_heads + head) * a.page_size + o;
+    };
+    half(0, r.off0, r.w0, r.there0);
+    half(1, r.off1, r.w1, r.there1);
+    return r;
+  }
+  // which of a tile's 32 keys lie on pages that are there
+  __device__ __forceinline__ uint32_t there(const Attn4Args& a, int tile) const {
+    if (!absent) return ~0u;
+    const int page = trow[min(entry4(a, tile * 32 + (lane_id() & 31)), e_last)];
+    return (uint32_t)__ballot(page >= 0 && page < a.pages);
+  }
+  __device__ __forceinline__ void copy(const Attn4Args& a, const At& at, int stage) const {
+    const lds_t to = lds + (uint32_t)stage * kStage;
+    if constexpr (D == 64) {
+      const uint64_t off = pick(lane_id() < 32, at.off0, at.off1);
+      copy16(to, k + off + k_off[0]);
+      if constexpr (VALUES) copy16(to + kV, v + off + v_off[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+        const uint64_t off = pick(i < KI / 2, at.off0, at.off1);
+        copy16(to + i * 1024, k + off, k_off[D == 256 ? i % 2 : 0]);
+        if constexpr (VALUES) copy16(to + kV + i * 1024, v + off, v_off[D == 256 ? i % 2 : 0]);
+      }
+    }
+    if constexpr (D <= 128) {  // keys' scales and values' at once
+      const uint64_t off = pick((lane_id() & 16) == 0, at.off0, at.off1) / 16 + s_off;
+      copy4<D == 64>(to + kS, pick(VALUES && lane_id() >= 32, vs, ks) + off);
+    } else {
+      const uint64_t off = pick(lane_id() < 32, at.off0, at.off1) / 16 + s_off;
+      copy4<false>(to + kS, ks + off);
+      if constexpr (VALUES) copy4<false>(to + kS + 256, vs + off);
+    }
+    if constexpr (!VALUES)
+      copy4<false>(to + kW, (const unsigned char*)(a.weights + pick((lane_id() & 16) == 0, at.w0, at.w1) + lane_id() % 16));
+  }
+  // a stage's operands
+  __device__ __forceinline__ void read(int stage, Raw4<C>& r) const {
+    typedef __attribute__((address_space(3))) uint16_t* lds_u16_t;
+    typedef __attribute__((address_space(3))) u32x2_t* lds_u32x2_t;
+    const lds_t at = lds + (uint32_t)stage * kStage;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if constexpr (D == 64) {
+        const u32x2_t w = *(lds_u32x2_t)(at + h * 16 * RB + k_at);
+        r.k[h][0] = w[0];
+        r.k[h][1] = w[1];
+      } else {
+#pragma unroll
+        for (int y = 0; y < C::KW / 4; ++y) {
+          const int g = lane_id() >> 4;
+          const u32x4_t w = *(lds_u32x4_t)(at + h * 16 * RB + k_at + ((g * (C::KW / 4) + y) ^ k_x) * 16);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r.k[h][4 * y + i] = w[i];
+        }
+      }
+      if constexpr (C::KS > 1) {
+        const uint32_t w = *(lds_u16_t)(at + ks_at + h * 16 * SB);
+        r.ks[h][0] = w & 0xff;
+        r.ks[h][1] = w >> 8;
+      } else {
+        r.ks[h][0] = *(at + ks_at + h * 16 * SB);
+      }
+    }
+    if constexpr (VALUES) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const lds_t from = at + v_at + ((e / 4) * 16 + (e % 4) * 4) * RB;
+        if constexpr (C::VB == 2) {
+          r.v[e][0] = *(lds_u16_t)from;
+        } else if constexpr (C::VB == 4) {
+          r.v[e][0] = *(lds_u32_t)from;
+        } else {
+          const u32x2_t w = *(lds_u32x2_t)from;
+          r.v[e][0] = w[0];
+          r.v[e][1] = w[1];
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if constexpr (D <= 128) {
+          const u32x4_t w = *(lds_u32x4_t)(at + vs_at + h * 16 * SB);
+          const uint32_t sh = (lane_id() & 15) / (D == 64 ? 8 : 4) * 8;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r.vs[4 * h + e] = w[e] >> sh & 0xff;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r.vs[4 * h + e] = *(at + vs_at + (16 * h + e) * SB);
+        }
+      }
+    }
+  }
+};
 
 // the h-th half's 16 keys as operands of the D / 32 score products
 template <typename C>
@@ -251,6 +432,15 @@ __device__ __forceinline__ void queries4(const uint16_t* at, int d, u32x4_t (&q)
   }
 }
 
+// Workgroup b, which runs on XCD b % 8, as an item: the head groups of a request's chunk come one after the other on one
+// XCD, so that they find the lines that they share in its L2, and the chunks go round the XCDs.
+__device__ __forceinline__ int beside(int b, int items, int head_groups) {
+  const int whole = items / head_groups / 8 * 8 * head_groups;
+  if (b >= whole) return b;
+  const int q = b / 8;
+  return (q / head_groups * 8 + b % 8) * head_groups + q % head_groups;
+}
+
 // Which rows a tile of BM has: request n, its first row r0 and the end r1 of them, first token, position of the first
 // query. False where there are none.
 struct Rows4 {
@@ -290,21 +480,19 @@ __device__ __forceinline__ bool rows4(const Attn4Args& a, int tile, Rows4& r) {
 }
 
 template <typename C>
-__global__ __launch_bounds__(C::kThreads) void attention4_kernel(Attn4Args a) {
+__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kSimdWaves, C::kSimdWaves)))
+void attention4_kernel(Attn4Args a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char attn4_smem[];
   typedef typename C::T T;
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = (int)uniform32(tid >> 6);
-  const int wr = wave % C::WR, wk = wave / C::WR;
+  const int wh = wave % C::WH, wr = wave / C::WH % C::WR, wk = wave / (C::WH * C::WR);
 
   // ---- which rows ------------------------------------------------------------------------------
-  int it = (int)blockIdx.x;
-  if (a.spread) {
-    const int per = a.items / 8;
-    if (it < per * 8) it = (it % 8) * per + it / 8;
-  }
-  const int head = it % a.kv_heads;
-  const int rest = it / a.kv_heads;
+  const int head_groups = a.kv_heads / C::WH;
+  const int it = a.spread ? beside((int)blockIdx.x, a.items, head_groups) : (int)blockIdx.x;
+  const int head = it % head_groups * C::WH + wh;
+  const int rest = it / head_groups;
   const int chunk_no = rest / a.tiles;
   Rows4 rw;
   // long rows first: with a causal mask and no window the last tiles of a request see most
@@ -345,16 +533,10 @@ __global__ __launch_bounds__(C::kThreads) void attention4_kernel(Attn4Args a) {
   const int wp_lo = rw.pos0 + min(wrow0, r1 - 1) / a.group;
   const int wp_hi = rw.pos0 + min(wrow0 + C::RT * 16 - 1, r1 - 1) / a.group;
 
-  Places4<C> pl;
-  pl.set(a);
   const int64_t ho = (int64_t)head * a.head_stride;
   const unsigned char *k = a.k + ho, *v = a.v + ho, *ks = a.ks + ho / 16, *vs = a.vs + ho / 16;
   const int32_t* trow = a.table + (int64_t)rw.n * a.table_width;
   auto tile_at = [&](int i) { return i < s_t ? i : i - s_t + t_lo; };
-  auto page_of = [&](int i) {  // of key lane % 32 of the list's tile i, or of the last one's last key
-    const int j = min(tile_at(min(i, t_end - 1)) * 32 + (lane & 31), hi - 1);
-    return trow[entry4(a, j)];
-  };
 
   f32x4_t o[C::RT][C::ND];
   float m[C::RT], l[C::RT], lu[C::RT];
@@ -368,10 +550,10 @@ __global__ __launch_bounds__(C::kThreads) void attention4_kernel(Attn4Args a) {
     poison[t] = 0;
   }
 
-  // one tile, `page` its keys' pages as the table has them
-  auto use = [&](Raw4<C>& r, int i, int page) __attribute__((always_inline)) {
+  // one tile; of its keys those in `there` are on pages that are there
+  auto use = [&](Raw4<C>& r, int i, uint32_t there) __attribute__((always_inline)) {
     const int j0 = tile_at(i) * 32;
-    const uint32_t here = (uint32_t)__ballot(page >= 0 && page < a.pages) & bits32_below(hi - j0);
+    const uint32_t here = there & bits32_below(hi - j0);
     const bool whole = here == ~0u && (!a.causal || j0 + 31 <= wp_lo) &&
                        (!a.window || j0 > wp_hi - a.window || j0 + 31 < a.sinks);
     uint32_t vis[C::RT];
@@ -500,26 +682,62 @@ __global__ __launch_bounds__(C::kThreads) void attention4_kernel(Attn4Args a) {
       product(std::integral_constant<int, 7>{});
     }
   };
-  auto place = [&](int page) { return page >= 0 && page < a.pages ? page : 0; };
-  auto load = [&](int i, int page, Raw4<C>& r) __attribute__((always_inline)) {
-    load4<C, true>(a, pl, k, v, ks, vs, tile_at(min(i, t_end - 1)), place(page), r);
-  };
-  // two sets of registers in turn: a tile is asked for while the one before it is used, its pages a tile earlier
   int i = t_begin + wk;
-  if (i < t_end) {
+  if constexpr (C::RING) {
+    Ring4<C, true> ring;
+    if (i < t_end) {
+      ring.set(a, k, v, ks, vs, trow, hi, (lds_t)attn4_smem + (uint32_t)wave * Ring4<C, true>::kBytes);
+      // tiles of this wave; NS - 1 of them are under way
+      const int tiles = (t_end - i + C::WK - 1) / C::WK;
+      auto find = [&](int s) { return ring.find(a, tile_at(i + min(s, tiles - 1) * C::WK)); };
+#pragma unroll
+      for (int s = 0; s < C::NS - 1; ++s)
+        if (s < tiles) ring.copy(a, find(s), s);
+      auto next = find(C::NS - 1);
+      int at = 0, to = C::NS - 1;
+      for (int s = 0; s < tiles; ++s) {
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last stage's reads, whose place is copied to next
+        if (s + C::NS - 1 < tiles) {
+          ring.copy(a, next, to);
+          __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NS - 1) * Ring4<C, true>::IPS) : "memory");
+        } else {
+          __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        Raw4<C> r;
+        ring.read(at, r);
+        if (s + C::NS < tiles) next = find(s + C::NS);
+        const int x = i + s * C::WK;
+        use(r, x, ring.there(a, tile_at(x)));
+        at = at + 1 == C::NS ? 0 : at + 1;
+        to = to + 1 == C::NS ? 0 : to + 1;
+      }
+    }
+    if constexpr (C::WK > 1) __syncthreads();  // the rings' memory is used again below
+  } else if (i < t_end) {
+    Places4<C> pl;
+    pl.set(a);
+    auto page_of = [&](int i) {  // of key lane % 32 of the list's tile i, or of the last one's last key
+      const int j = min(tile_at(min(i, t_end - 1)) * 32 + (lane & 31), hi - 1);
+      return trow[entry4(a, j)];
+    };
+    auto there = [&](int page) { return (uint32_t)__ballot(page >= 0 && page < a.pages); };
+    auto load = [&](int i, int page, Raw4<C>& r) __attribute__((always_inline)) {
+      load4<C, true>(a, pl, k, v, ks, vs, tile_at(min(i, t_end - 1)), page >= 0 && page < a.pages ? page : 0, r);
+    };
+    // two sets of registers in turn: a tile is asked for while the one before it is used, its pages a tile earlier
     Raw4<C> ra, rb;
     int pa = page_of(i), pb = page_of(i + C::WK);
     load(i, pa, ra);
     while (true) {
       int next = page_of(i + 2 * C::WK);
       load(i + C::WK, pb, rb);
-      use(ra, i, pa);
+      use(ra, i, there(pa));
       pa = next;
       i += C::WK;
       if (i >= t_end) break;
       next = page_of(i + 2 * C::WK);
       load(i + C::WK, pa, ra);
-      use(rb, i, pb);
+      use(rb, i, there(pb));
       pb = next;
       i += C::WK;
       if (i >= t_end) break;
@@ -555,7 +773,7 @@ __global__ __launch_bounds__(C::kThreads) void attention4_kernel(Attn4Args a) {
       float f[C::WK], top = -__builtin_inff();
 #pragma unroll
       for (int w = 0; w < C::WK; ++w) {
-        ml[w] = *(lds_f32x4_t)(attn4_smem + C::kOut + (((w * C::WR + wr) * C::RT + t) * kWave + lane) * 16);
+        ml[w] = *(lds_f32x4_t)(attn4_smem + C::kOut + ((((w * C::WR + wr) * C::WH + wh) * C::RT + t) * kWave + lane) * 16);
         top = fmaxf(top, ml[w][0]);
       }
       l[t] = lu[t] = 0.f;
@@ -572,7 +790,7 @@ __global__ __launch_bounds__(C::kThreads) void attention4_kernel(Attn4Args a) {
         f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < C::WK; ++w)
-          sum += f[w] * *(lds_f32x4_t)(attn4_smem + ((((w * C::WR + wr) * C::RT + t) * C::ND + i) * kWave + lane) * 16);
+          sum += f[w] * *(lds_f32x4_t)(attn4_smem + (((((w * C::WR + wr) * C::WH + wh) * C::RT + t) * C::ND + i) * kWave + lane) * 16);
         o[t][i] = sum;
       }
     }
@@ -692,15 +910,13 @@ __device__ __forceinline__ int64_t weight_at(const Attn4Args& a, int page, int h
 // additions and two exchanges.
 template <typename C>
 __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char attn4_smem[];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
-  const int wk = (int)uniform32(tid >> 6);
-  int it = (int)blockIdx.x;
-  if (a.spread) {
-    const int per = a.items / 8;
-    if (it < per * 8) it = (it % 8) * per + it / 8;
-  }
-  const int head = it % a.kv_heads;
-  const int rest = it / a.kv_heads;
+  const int wave = (int)uniform32(tid >> 6), wh = wave % C::WH, wk = wave / C::WH;
+  const int head_groups = a.kv_heads / C::WH;
+  const int it = a.spread ? beside((int)blockIdx.x, a.items, head_groups) : (int)blockIdx.x;
+  const int head = it % head_groups * C::WH + wh;
+  const int rest = it / head_groups;
   const int chunk_no = rest / a.tiles;
   Rows4 rw;
   if (!rows4<16>(a, rest % a.tiles, rw) || rw.T > a.max_tokens) return;
@@ -723,22 +939,11 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args 
     ls[r] = x >= rw.r1 || v == -__builtin_inff() ? __builtin_inff() : v * 1.4426950408889634f;
     p[r] = rw.pos0 + tok;
   }
-  Places4<C> pl;
-  pl.set(a);
   const int64_t ho = (int64_t)head * a.head_stride;
   const unsigned char *k = a.k + ho, *ks = a.ks + ho / 16;
   const int32_t* trow = a.table + (int64_t)rw.n * a.table_width;
-  auto page_of = [&](int x) {
-    const int j = min(min(x, t_end - 1) * 32 + (lane & 31), hi - 1);
-    return trow[entry4(a, j)];
-  };
-  auto place = [&](int page) { return page >= 0 && page < a.pages ? page : 0; };
-  auto load = [&](int x, int page, Raw4<C>& r, float& w) __attribute__((always_inline)) {
-    x = min(x, t_end - 1);
-    load4<C, false>(a, pl, k, k, ks, ks, x, place(page), r);
-    w = a.weights[weight_at(a, place(page), head, x * 32 + (lane & 31))];
-  };
-  auto use = [&](const Raw4<C>& r, float before, int x, int page) __attribute__((always_inline)) {
+  // the new weight of key lane % 32 of tile x
+  auto use = [&](const Raw4<C>& r, float before, int x) __attribute__((always_inline)) {
     const int j0 = x * 32;
     const bool all = !a.causal || j0 + 31 <= rw.pos0;
     float got[2];
@@ -759,27 +964,79 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args 
       }
       got[h] = quad_sum((e[0] + e[1]) + (e[2] + e[3]));
     }
-    const int j = j0 + lane;  // lanes 0 .. 31
-    if (lane < 32 && j < hi && page >= 0 && page < a.pages)
-      a.weights[weight_at(a, page, head, j)] = (j < rw.pos0 ? a.decay * before : 0.f) + (lane < 16 ? got[0] : got[1]);
+    return (j0 + (lane & 31) < rw.pos0 ? a.decay * before : 0.f) + ((lane & 16) ? got[1] : got[0]);
   };
-  Raw4<C> ra, rb;
-  float wa, wb;
-  int pa = page_of(i), pb = page_of(i + C::WK);
-  load(i, pa, ra, wa);
-  while (true) {
-    int next = page_of(i + 2 * C::WK);
-    load(i + C::WK, pb, rb, wb);
-    use(ra, wa, i, pa);
-    pa = next;
-    i += C::WK;
-    if (i >= t_end) break;
-    next = page_of(i + 2 * C::WK);
-    load(i + C::WK, pa, ra, wa);
-    use(rb, wb, i, pb);
-    pb = next;
-    i += C::WK;
-    if (i >= t_end) break;
+  auto page_of = [&](int x) {
+    const int j = min(min(x, t_end - 1) * 32 + (lane & 31), hi - 1);
+    return trow[entry4(a, j)];
+  };
+  auto place = [&](int page) { return page >= 0 && page < a.pages ? page : 0; };
+  auto old = [&](int x, int page) {
+    return a.weights[weight_at(a, place(page), head, min(x, t_end - 1) * 32 + (lane & 31))];
+  };
+  if constexpr (C::RING) {
+    typedef Ring4<C, false> Ring;
+    Ring ring;
+    ring.set(a, k, k, ks, ks, trow, hi, (lds_t)attn4_smem + (uint32_t)wave * Ring::kBytes);
+    const int tiles = (t_end - i + C::WK - 1) / C::WK;
+    auto find = [&](int s) { return ring.find(a, i + min(s, tiles - 1) * C::WK, head); };
+    typename Ring::At where[C::NS + 1];  // of the tiles under way, this one first
+#pragma unroll
+    for (int s = 0; s <= C::NS - 1; ++s) {
+      where[s] = find(s);
+      if (s < C::NS - 1 && s < tiles) ring.copy(a, where[s], s);
+    }
+    int at = 0, to = C::NS - 1;
+    for (int s = 0; s < tiles; ++s) {
+      __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (s + C::NS - 1 < tiles) {
+        ring.copy(a, where[C::NS - 1], to);
+        __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NS - 1) * Ring::IPS) : "memory");
+      } else {
+        __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+      Raw4<C> r;
+      ring.read(at, r);
+      const float before = *(lds_float_t)(ring.lds + (uint32_t)at * Ring::kStage + Ring::kW + (lane & 31) * 4);
+      where[C::NS] = find(s + C::NS);
+      const int x = i + s * C::WK;
+      const float w = use(r, before, x);
+      if (lane < 32 && x * 32 + lane < hi && pick((lane & 16) == 0, where[0].there0, where[0].there1))
+        a.weights[pick((lane & 16) == 0, where[0].w0, where[0].w1) + (lane & 15)] = w;
+#pragma unroll
+      for (int y = 0; y < C::NS; ++y) where[y] = where[y + 1];
+      at = at + 1 == C::NS ? 0 : at + 1;
+      to = to + 1 == C::NS ? 0 : to + 1;
+    }
+  } else {
+    Places4<C> pl;
+    pl.set(a);
+    auto load = [&](int x, int page, Raw4<C>& r, float& w) __attribute__((always_inline)) {
+      load4<C, false>(a, pl, k, k, ks, ks, min(x, t_end - 1), place(page), r);
+      w = old(x, page);
+    };
+    auto store = [&](int x, int page, float w) {
+      const int j = x * 32 + lane;
+      if (lane < 32 && j < hi && page >= 0 && page < a.pages) a.weights[weight_at(a, page, head, j)] = w;
+    };
+    Raw4<C> ra, rb;
+    float wa, wb;
+    int pa = page_of(i), pb = page_of(i + C::WK);
+    load(i, pa, ra, wa);
+    while (true) {
+      int next = page_of(i + 2 * C::WK);
+      load(i + C::WK, pb, rb, wb);
+      store(i, pa, use(ra, wa, i));
+      pa = next;
+      i += C::WK;
+      if (i >= t_end) break;
+      next = page_of(i + 2 * C::WK);
+      load(i + C::WK, pa, ra, wa);
+      store(i, pb, use(rb, wb, i));
+      pb = next;
+      i += C::WK;
+      if (i >= t_end) break;
+    }
   }
 }
 

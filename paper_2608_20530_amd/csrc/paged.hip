@@ -752,7 +752,7 @@ extern "C" lilicorr_status lilicorr_qk_norm_rope4(const lilicorr_qk_norm_rope4_a
   // q rows that are turned in place must be laid out as the output is
   if (x.q_out == x.q && x.tokens > 1 && x.q_stride != (int64_t)x.heads * c.d) return LILICORR_ERR_INVALID_ARG;
   if (!aligned16(x.q) || !aligned16(x.k) || !aligned16(x.v) || !aligned16(x.q_out) || !aligned16(c.k) ||
-      !aligned16(c.v) || !aligned16(x.cos_sin) || !aligned16(x.q_weight) || !aligned16(x.k_weight) ||
+      !aligned16(c.v) || !aligned4(c.k_scales) || !aligned4(c.v_scales) || !aligned16(x.cos_sin) || !aligned16(x.q_weight) || !aligned16(x.k_weight) ||
       !aligned4(x.slots) || !aligned4(x.positions))
     return LILICORR_ERR_ALIGNMENT;
   // what other waves still read must not lie where q_out does, nor q_out in the cache
