@@ -40,7 +40,7 @@ void with_rows4(int BM, bool heads, const F& use) {
       if (BM == 16) return use(Attn4Config<T, D, 1, 4, 1, 1, RING>());
       if constexpr (D <= 128) {
         if (BM == 32) return use(Attn4Config<T, D, 2, 4, 1, 1, RING>());
-        if (BM == 64) return use(Attn4Config<T, D, 2, 2, 2, 1, RING>());
+        if (BM == 64) return use(Attn4Config<T, D, 4, 4, 1, 1, RING>());
       } else {
         if (BM == 32) return use(Attn4Config<T, D, 1, 2, 2, 1, RING>());
       }
@@ -121,7 +121,7 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
   p.ring = ring_fits(a.cache);
   p.spread = own <= p.BM;
   // key heads over the waves, where that still leaves every compute unit work
-  const int wide = p.BM <= 16 || (p.BM == 32 && a.cache.d <= 128) ? 4 : p.BM <= 64 && (a.cache.d <= 128 || p.BM == 32) ? 2 : 1;
+  const int wide = p.BM <= 16 || (p.BM <= 64 && a.cache.d <= 128) ? 4 : p.BM <= 64 && (a.cache.d <= 128 || p.BM == 32) ? 2 : 1;
   const int64_t pairs = tiles * a.cache.heads;
   p.heads = p.ring && wide > 1 && a.cache.heads % wide == 0 && pairs * most >= LEAST_TILES ? wide : 1;
   const int64_t items = pairs / p.heads, wk = p.heads > 1 ? 1 : p.BM <= 32 ? (p.BM == 32 && a.cache.d > 128 ? 2 : 4) : p.BM == 64 && a.cache.d <= 128 ? 2 : 1;

@@ -78,7 +78,14 @@ struct Attn4Config {
   static constexpr int RT = RT_;  // blocks of 16 rows of a wave
   static constexpr int WH = WH_, WR = WR_, WK = WK_;  // waves of key heads by waves of rows by waves of keys
   static constexpr bool RING = RING_;  // tiles by way of LDS
-  static constexpr int NS = D <= 64 ? 4 : D <= 128 ? 3 : 2;  // stages of a wave's ring
+#ifndef SIMD1
+#define SIMD1 3
+#endif
+#ifndef NS1
+#define NS1 3
+#define NS4 4
+#endif
+  static constexpr int NS = RT == 4 ? (D <= 64 ? 10 : NS4) : D <= 64 ? 4 : D <= 128 ? NS1 : 2;  // stages of a wave's ring
   static constexpr int kWaves = WH * WR * WK, kThreads = kWaves * kWave;
   static constexpr int BM = 16 * RT * WR;
   static constexpr int ND = D / 16;  // output products
@@ -92,7 +99,7 @@ struct Attn4Config {
   // waves of a SIMD that the registers are given out for: two or more keep the accumulators where the vector unit
   // reaches them
   static constexpr int kSimdWaves =
-      D > 128 || RT == 4 || (RT == 2 && D > 64 && kTerms > 1) ? 1 : RT == 1 && kTerms == 1 ? 3 : 2;
+      D > 128 || RT == 4 || (RT == 2 && D > 64 && kTerms > 1) ? 1 : RT == 1 && kTerms == 1 ? SIMD1 : 2;
 };
 
 // What a wave has under way of a tile of 32 keys
@@ -226,8 +233,8 @@ struct Ring4 {
   static constexpr uint32_t kStage = kS + (D <= 128 && VALUES ? 256 : 512);
   static constexpr int IPS = KI * (VALUES ? 2 : 1) + (D <= 128 && VALUES ? 1 : 2);  // copies of a stage
   static constexpr int NS = C::NS;
-  static constexpr int kEntries = 128;            // of the page table, which the wave keeps
-  static constexpr uint32_t kBytes = NS * kStage + kEntries * 4;
+    static constexpr uint32_t kBytes = NS * kStage;
+  static constexpr int kBatch = kWave / 2;        // tiles whose places the lanes have, a half each
 
   const unsigned char *k, *v, *ks, *vs;
   const int32_t* trow;
@@ -235,8 +242,13 @@ struct Ring4 {
   uint32_t k_off[2], v_off[2];  // of a lane's piece: bytes
   uint32_t s_off;
   uint32_t k_at, k_x, v_at, ks_at, vs_at;  // LDS offsets of its reads
-  int x0, e_last;               // first entry that is kept, last one that there is
-  bool absent;                  // a page among those so far is not there
+  int e_last;                   // last entry that there is
+  int base;                     // first tile of the batch
+  uint64_t off;                 // of this lane's half: bytes of codes from the head's first
+  int64_t w;                    // and its first key's weight, without values
+  uint64_t valid;               // the halves whose page is there
+  uint32_t ahead;               // page of the next batch's half
+  uint64_t seen;                // two bits a tile that was found, the last one's lowest
 
   __device__ __forceinline__ void set(const Attn4Args& a, const unsigned char* k_, const unsigned char* v_,
                                       const unsigned char* ks_, const unsigned char* vs_, const int32_t* trow_,
@@ -258,56 +270,67 @@ struct Ring4 {
     v_at = kV + g * RB + c * C::VB;
     ks_at = kS + c * SB + (D == 64 ? g / 2 : D == 128 ? g : 2 * g);
     vs_at = kS + 32 * SB + 4 * g * SB + (D > 128 ? c / 2 : 0);
-    x0 = -kEntries;
-    absent = false;
     e_last = entry4(a, keys - 1);
   }
   static __device__ __forceinline__ uint32_t swizzle(int r) {
     return D == 64 ? (r >> 3) & 1 : D == 128 ? (r >> 2) & 3 : (r >> 1) & 7;
   }
 
-  // offsets (bytes of codes) of the two halves of the tile of 32 keys from `tile`'s first on
+  // offsets (bytes of codes) of the two halves of a tile
   struct At {
     uint64_t off0, off1;
-    int64_t w0, w1;      // of the first key's weight, without values
-    bool there0, there1; // whether the page is there
+    int64_t w0, w1;       // without values
   };
-  __device__ __forceinline__ At find(const Attn4Args& a, int tile, int head = 0) {
-    const int e0 = min(entry4(a, tile * 32), e_last), e1 = min(entry4(a, tile * 32 + 16), e_last);
-    const lds_u32_t kept = (lds_u32_t)(lds + NS * kStage);
-    if (e0 < x0 || e1 >= x0 + kEntries) {  // (uniform)
-      x0 = e0;
-      uint32_t page[kEntries / kWave];
-      bool gone = false;
-#pragma unroll
-      for (int u = 0; u < kEntries / kWave; ++u) page[u] = (uint32_t)trow[min(x0 + u * kWave + lane_id(), e_last)];
-#pragma unroll
-      for (int u = 0; u < kEntries / kWave; ++u) {
-        gone |= page[u] >= (uint32_t)a.pages;
-        kept[u * kWave + lane_id()] = page[u];
-      }
-      absent |= __ballot(gone) != 0;
-    }
-    const uint32_t pages = kept[(lane_id() < 32 ? e0 : e1) - x0];
+  // The s-th of `tiles` tiles, the number of which in the sequence tile_of gives; one after the other. 64 lanes work the
+  // places of 32 tiles out at once, which costs a tile four v_readlane (a tile's places by scalar instructions
+  // were 70 of them, one after the other).
+  template <typename F>
+  __device__ __forceinline__ int entry_at(const Attn4Args& a, int first, int tiles, const F& tile_of, int& j) const {
+    j = tile_of(min(first + lane_id() / 2, tiles - 1)) * 32 + 16 * (lane_id() & 1);
+    return min(entry4(a, j), e_last);
+  }
+  template <typename F>
+  __device__ __forceinline__ void batch(const Attn4Args& a, int first, int tiles, const F& tile_of, int head) {
+    base = first;
+    int j;
+    entry_at(a, base, tiles, tile_of, j);
+    uint32_t page = ahead;
+    valid = __ballot(page < (uint32_t)a.pages);
+    if (page >= (uint32_t)a.pages) page = 0;
+    const uint32_t o = (uint32_t)j - (uint32_t)entry4(a, j) * a.page_size;
+    off = (uint64_t)page * (uint64_t)a.page_stride + (uint64_t)o * (uint64_t)a.token_stride;
+    if constexpr (!VALUES) w = ((int64_t)page * a.kv_heads + head) * a.page_size + o;
+    if (base + kBatch < tiles) ahead = (uint32_t)trow[entry_at(a, base + kBatch, tiles, tile_of, j)];
+  }
+  // before the first find(): everything that has been asked for so far is there afterwards, so that the compiler puts no
+  // wait for it among the copies, which it does not see
+  template <typename F>
+  __device__ __forceinline__ void begin(const Attn4Args& a, int tiles, const F& tile_of, int head = 0) {
+    int j;
+    ahead = (uint32_t)trow[entry_at(a, 0, tiles, tile_of, j)];
+    seen = 0;
+    batch(a, 0, tiles, tile_of, head);
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0) alone
+  }
+  template <typename F>
+  __device__ __forceinline__ At find(const Attn4Args& a, int s, int tiles, const F& tile_of, int head = 0) {
+    s = min(s, tiles - 1);
+    if (__builtin_expect(s >= base + kBatch, 0)) batch(a, base + kBatch, tiles, tile_of, head);
+    const int q = 2 * (s - base);
     At r;
-    auto half = [&](int h, uint64_t& off, int64_t& w, bool& there) __attribute__((always_inline)) {
-      const int j = tile * 32 + 16 * h;
-      uint32_t page = readlane32(pages, 32 * h);
-      there = page < (uint32_t)a.pages;
-      page = there ? page : 0;
-      const uint32_t o = (uint32_t)j - (uint32_t)entry4(a, j) * a.page_size;
-      off = (uint64_t)page * (uint64_t)a.page_stride + (uint64_t)o * (uint64_t)a.token_stride;
-      w = VALUES ? 0 : ((int64_t)page * a.kv_heads + head) * a.page_size + o;
-    };
-    half(0, r.off0, r.w0, r.there0);
-    half(1, r.off1, r.w1, r.there1);
+    r.off0 = readlane64(off, q);
+    r.off1 = readlane64(off, q + 1);
+    if constexpr (!VALUES) {
+      r.w0 = (int64_t)readlane64((uint64_t)w, q);
+      r.w1 = (int64_t)readlane64((uint64_t)w, q + 1);
+    }
+    seen = seen << 2 | (valid >> q & 3);
     return r;
   }
-  // which of a tile's 32 keys lie on pages that are there
-  __device__ __forceinline__ uint32_t there(const Attn4Args& a, int tile) const {
-    if (!absent) return ~0u;
-    const int page = trow[min(entry4(a, tile * 32 + (lane_id() & 31)), e_last)];
-    return (uint32_t)__ballot(page >= 0 && page < a.pages);
+  // which of the 32 keys of the tile that was found `back` tiles before the last one lie on pages that are there
+  __device__ __forceinline__ uint32_t there(int back) const {
+    const uint32_t b = (uint32_t)(seen >> (2 * back));
+    return ((b & 1) ? 0xffffu : 0u) | ((b & 2) ? 0xffff0000u : 0u);
   }
   __device__ __forceinline__ void copy(const Attn4Args& a, const At& at, int stage) const {
     const lds_t to = lds + (uint32_t)stage * kStage;
@@ -532,6 +555,9 @@ void attention4_kernel(Attn4Args a) {
   const int wrow0 = r0 + wr * C::RT * 16;
   const int wp_lo = rw.pos0 + min(wrow0, r1 - 1) / a.group;
   const int wp_hi = rw.pos0 + min(wrow0 + C::RT * 16 - 1, r1 - 1) / a.group;
+  // all of the wave's rows see all keys of the tiles below whole_to, from whole_from on or below whole_sinks
+  const int whole_to = max(a.causal ? min(hi, wp_lo + 1) : hi, 0) / 32;
+  const int whole_from = a.window ? max(wp_hi - a.window + 32, 0) / 32 : 0, whole_sinks = a.window ? a.sinks / 32 : 0;
 
   const int64_t ho = (int64_t)head * a.head_stride;
   const unsigned char *k = a.k + ho, *v = a.v + ho, *ks = a.ks + ho / 16, *vs = a.vs + ho / 16;
@@ -550,12 +576,12 @@ void attention4_kernel(Attn4Args a) {
     poison[t] = 0;
   }
 
-  // one tile; of its keys those in `there` are on pages that are there
-  auto use = [&](Raw4<C>& r, int i, uint32_t there) __attribute__((always_inline)) {
-    const int j0 = tile_at(i) * 32;
-    const uint32_t here = there & bits32_below(hi - j0);
-    const bool whole = here == ~0u && (!a.causal || j0 + 31 <= wp_lo) &&
-                       (!a.window || j0 > wp_hi - a.window || j0 + 31 < a.sinks);
+  // One tile, whose keys all rows see (`whole`) or not: `here` are those that there are. False, and nothing accumulated,
+  // where a maximum has grown too far over its reference: then grow(), and again. The accumulators change
+  // outside the loop over the tiles, since the compiler copies them at every join of paths inside it (38 moves a tile with
+  // two blocks of rows, 144 with four).
+  float mx[C::RT];
+  auto step = [&](Raw4<C>& r, int j0, uint32_t here, bool whole) __attribute__((always_inline)) -> bool {
     uint32_t vis[C::RT];
     if (!whole) {
 #pragma unroll
@@ -579,7 +605,7 @@ void attention4_kernel(Attn4Args a) {
           for (int u = 0; u < C::kTerms; ++u) sc[t][h] = mfma16(kk[w], q[t][u][w], sc[t][h]);
       }
     }
-    u32x4_t pf[C::RT][C::kTerms];
+    bool up = false;
 #pragma unroll
     for (int t = 0; t < C::RT; ++t) {
       if (!whole) {
@@ -588,25 +614,16 @@ void attention4_kernel(Attn4Args a) {
         for (int e = 0; e < 8; ++e)
           sc[t][e / 4][e % 4] = mine & (1u << (16 * (e / 4) + e % 4)) ? sc[t][e / 4][e % 4] : -__builtin_inff();
       }
-      float mx = max3(sc[t][0][0], sc[t][0][1], sc[t][0][2]);
-      mx = max3(mx, sc[t][0][3], sc[t][1][0]);
-      mx = max3(mx, sc[t][1][1], sc[t][1][2]);
-      mx = max3(mx, sc[t][1][3], mx);
-      // -inf - -inf is NaN and does not count
-      if (__ballot(fmaf(mx, a.scale2, -m[t]) > kRescale4)) {
-        mx = quad_max(mx);
-        const bool grows = fmaf(mx, a.scale2, -m[t]) > kRescale4;
-        const float up = __builtin_floorf(mx * a.scale2);
-        // nothing is accumulated while m is -inf
-        const float f = grows ? __builtin_amdgcn_ldexpf(1.f, (int)fmaxf(m[t] - up, -300.f)) : 1.f;
-        m[t] = grows ? up : m[t];
-        l[t] *= f;
-        lu[t] *= f;
+      mx[t] = max3(sc[t][0][0], sc[t][0][1], sc[t][0][2]);
+      mx[t] = max3(mx[t], sc[t][0][3], sc[t][1][0]);
+      mx[t] = max3(mx[t], sc[t][1][1], sc[t][1][2]);
+      mx[t] = max3(mx[t], sc[t][1][3], mx[t]);
+      up |= fmaf(mx[t], a.scale2, -m[t]) > kRescale4;  // -inf - -inf is NaN and does not count
+    }
+    if (__builtin_expect(__ballot(up) != 0, 0)) return false;
+    u32x4_t pf[C::RT][C::kTerms];
 #pragma unroll
-        for (int i = 0; i < C::ND; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[t][i][e] *= f;
-      }
+    for (int t = 0; t < C::RT; ++t) {
       const float ms = m[t] == -__builtin_inff() ? 0.f : m[t];
       float e[8];
 #pragma unroll
@@ -632,7 +649,7 @@ void attention4_kernel(Attn4Args a) {
       uint32_t top = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = max(top, r.vs[e]);
-      if (__ballot(top > kMostScale)) {
+      if (__builtin_expect(__ballot(top > kMostScale) != 0, 0)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint64_t bad = __ballot(r.vs[e] > kMostScale);
@@ -681,35 +698,64 @@ void attention4_kernel(Attn4Args a) {
       product(std::integral_constant<int, 6>{});
       product(std::integral_constant<int, 7>{});
     }
+    return true;
+  };
+  auto grow = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t) {
+      const float top = quad_max(mx[t]);
+      const bool grows = fmaf(top, a.scale2, -m[t]) > kRescale4;
+      const float to = __builtin_floorf(top * a.scale2);
+      // nothing is accumulated while m is -inf
+      const float f = grows ? __builtin_amdgcn_ldexpf(1.f, (int)fmaxf(m[t] - to, -300.f)) : 1.f;
+      m[t] = grows ? to : m[t];
+      l[t] *= f;
+      lu[t] *= f;
+#pragma unroll
+      for (int i = 0; i < C::ND; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[t][i][e] *= f;
+    }
+  };
+  // one tile; of its keys those in `there` are on pages that are there
+  auto use = [&](Raw4<C>& r, int i, uint32_t there) __attribute__((always_inline)) -> bool {
+    const int tile = tile_at(i), j0 = tile * 32;
+    const bool whole = there == ~0u && tile < whole_to && (tile >= whole_from || tile < whole_sinks);
+    return step(r, j0, there & bits32_below(hi - j0), whole);
   };
   int i = t_begin + wk;
   if constexpr (C::RING) {
     Ring4<C, true> ring;
     if (i < t_end) {
       ring.set(a, k, v, ks, vs, trow, hi, (lds_t)attn4_smem + (uint32_t)wave * Ring4<C, true>::kBytes);
-      // tiles of this wave; NS - 1 of them are under way
-      const int tiles = (t_end - i + C::WK - 1) / C::WK;
-      auto find = [&](int s) { return ring.find(a, tile_at(i + min(s, tiles - 1) * C::WK)); };
+      const int tiles = (t_end - i + C::WK - 1) / C::WK;  // of this wave; NS of them are under way
+      auto tile_of = [&](int s) { return tile_at(i + s * C::WK); };
+      auto find = [&](int s) { return ring.find(a, s, tiles, tile_of); };
+      ring.begin(a, tiles, tile_of);
 #pragma unroll
-      for (int s = 0; s < C::NS - 1; ++s)
-        if (s < tiles) ring.copy(a, find(s), s);
-      auto next = find(C::NS - 1);
-      int at = 0, to = C::NS - 1;
-      for (int s = 0; s < tiles; ++s) {
-        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last stage's reads, whose place is copied to next
-        if (s + C::NS - 1 < tiles) {
-          ring.copy(a, next, to);
-          __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NS - 1) * Ring4<C, true>::IPS) : "memory");
-        } else {
-          __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      for (int s = 0; s < C::NS; ++s) {
+        const auto first = find(s);
+        if (s < tiles) ring.copy(a, first, s);
+      }
+      auto next = find(C::NS);
+      int at = 0, s = 0;
+      while (true) {
+        for (; s < tiles; ++s) {
+          if (s + C::NS - 1 < tiles)
+            __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NS - 1) * Ring4<C, true>::IPS) : "memory");
+          else
+            __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          Raw4<C> r;
+          ring.read(at, r);
+          const int x = i + s * C::WK;
+          if (!use(r, x, ring.there(C::NS))) break;
+          __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this stage's reads, whose place is copied to next
+          if (s + C::NS < tiles) ring.copy(a, next, at);
+          next = find(s + C::NS + 1);
+          at = at + 1 == C::NS ? 0 : at + 1;
         }
-        Raw4<C> r;
-        ring.read(at, r);
-        if (s + C::NS < tiles) next = find(s + C::NS);
-        const int x = i + s * C::WK;
-        use(r, x, ring.there(a, tile_at(x)));
-        at = at + 1 == C::NS ? 0 : at + 1;
-        to = to + 1 == C::NS ? 0 : to + 1;
+        if (s >= tiles) break;
+        grow();
       }
     }
     if constexpr (C::WK > 1) __syncthreads();  // the rings' memory is used again below
@@ -731,13 +777,13 @@ void attention4_kernel(Attn4Args a) {
     while (true) {
       int next = page_of(i + 2 * C::WK);
       load(i + C::WK, pb, rb);
-      use(ra, i, there(pa));
+      while (!use(ra, i, there(pa))) grow();
       pa = next;
       i += C::WK;
       if (i >= t_end) break;
       next = page_of(i + 2 * C::WK);
       load(i + C::WK, pa, ra);
-      use(rb, i, there(pb));
+      while (!use(rb, i, there(pb))) grow();
       pb = next;
       i += C::WK;
       if (i >= t_end) break;
@@ -979,7 +1025,9 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args 
     Ring ring;
     ring.set(a, k, k, ks, ks, trow, hi, (lds_t)attn4_smem + (uint32_t)wave * Ring::kBytes);
     const int tiles = (t_end - i + C::WK - 1) / C::WK;
-    auto find = [&](int s) { return ring.find(a, i + min(s, tiles - 1) * C::WK, head); };
+    auto tile_of = [&](int s) { return i + s * C::WK; };
+    auto find = [&](int s) { return ring.find(a, s, tiles, tile_of, head); };
+    ring.begin(a, tiles, tile_of, head);
     typename Ring::At where[C::NS + 1];  // of the tiles under way, this one first
 #pragma unroll
     for (int s = 0; s <= C::NS - 1; ++s) {
@@ -999,9 +1047,10 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args 
       ring.read(at, r);
       const float before = *(lds_float_t)(ring.lds + (uint32_t)at * Ring::kStage + Ring::kW + (lane & 31) * 4);
       where[C::NS] = find(s + C::NS);
+      const uint32_t there = ring.there(C::NS);
       const int x = i + s * C::WK;
       const float w = use(r, before, x);
-      if (lane < 32 && x * 32 + lane < hi && pick((lane & 16) == 0, where[0].there0, where[0].there1))
+      if (lane < 32 && x * 32 + lane < hi && (there >> lane & 1))
         a.weights[pick((lane & 16) == 0, where[0].w0, where[0].w1) + (lane & 15)] = w;
 #pragma unroll
       for (int y = 0; y < C::NS; ++y) where[y] = where[y + 1];
