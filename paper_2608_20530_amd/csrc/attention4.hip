@@ -40,7 +40,11 @@ void with_rows4(int BM, bool heads, const F& use) {
       if (BM == 16) return use(Attn4Config<T, D, 1, 4, 1, 1, RING>());
       if constexpr (D <= 128) {
         if (BM == 32) return use(Attn4Config<T, D, 2, 4, 1, 1, RING>());
+#ifdef B64
         if (BM == 64) return use(Attn4Config<T, D, 4, 4, 1, 1, RING>());
+#else
+        if (BM == 64) return use(Attn4Config<T, D, 2, 2, 2, 1, RING>());
+#endif
       } else {
         if (BM == 32) return use(Attn4Config<T, D, 1, 2, 2, 1, RING>());
       }
@@ -97,6 +101,11 @@ bool ring_fits(const lilicorr_cache4& c) {
   return even(c.page_stride) && even(c.token_stride) && even(c.head_stride);
 }
 
+// whether a token's heads lie side by side, with scales where 4-byte copies want them
+bool heads_together(const lilicorr_cache4& c) {
+  return c.head_stride == c.d / 2 && c.page_stride % 64 == 0 && c.token_stride % 64 == 0;
+}
+
 lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
   if (const lilicorr_status s = sizes4(a)) return s;
   if (a.window < 0 || a.sinks < 0 || (a.sinks > 0 && a.window == 0)) return LILICORR_ERR_INVALID_ARG;
@@ -121,9 +130,14 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
   p.ring = ring_fits(a.cache);
   p.spread = own <= p.BM;
   // key heads over the waves, where that still leaves every compute unit work
-  const int wide = p.BM <= 16 || (p.BM <= 64 && a.cache.d <= 128) ? 4 : p.BM <= 64 && (a.cache.d <= 128 || p.BM == 32) ? 2 : 1;
+#ifdef B64
+  const int most_rows = 64;
+#else
+  const int most_rows = 32;
+#endif
+  const int wide = p.BM <= 16 || (p.BM <= most_rows && a.cache.d <= 128) ? 4 : p.BM <= 64 && (a.cache.d <= 128 || p.BM == 32) ? 2 : 1;
   const int64_t pairs = tiles * a.cache.heads;
-  p.heads = p.ring && wide > 1 && a.cache.heads % wide == 0 && pairs * most >= LEAST_TILES ? wide : 1;
+  p.heads = p.ring && wide > 1 && a.cache.heads % wide == 0 && heads_together(a.cache) && pairs * most >= LEAST_TILES ? wide : 1;
   const int64_t items = pairs / p.heads, wk = p.heads > 1 ? 1 : p.BM <= 32 ? (p.BM == 32 && a.cache.d > 128 ? 2 : 4) : p.BM == 64 && a.cache.d <= 128 ? 2 : 1;
   int64_t chunk, chunks;
   if (p.heads > 1) {
@@ -169,9 +183,17 @@ Attn4Args common4(const A& x) {
   return a;
 }
 
+// LDS of a workgroup's tiles
+template <typename C, bool VALUES>
+constexpr uint32_t ring_bytes() {
+  if constexpr (!C::RING) return 0;
+  else if constexpr (C::WK == 1) return Shared4<C, VALUES>::kBytes;
+  else return C::kWaves * Ring4<C, VALUES>::kBytes;
+}
+
 template <typename C>
 void launch4(const Attn4Args& a, hipStream_t stream) {
-  constexpr uint32_t kRing = C::RING ? C::kWaves * Ring4<C, true>::kBytes : 0;
+  constexpr uint32_t kRing = ring_bytes<C, true>();
   constexpr uint32_t kLds = kRing > C::kJoin ? kRing : C::kJoin;
   static_assert(kLds <= 160 * 1024, "a workgroup fits");
   if constexpr (kLds > 65536) {
@@ -214,7 +236,7 @@ lilicorr_status run4(const lilicorr_attention4_args& x, const Plan4& p, hipStrea
 
 // keys of a tile of key_weights_many_kernel: WK waves of 64
 template <typename T, bool RING>
-void launch_weights(Attn4Args a, int d, hipStream_t stream) {
+void launch_weights(Attn4Args a, int d, bool heads_together, hipStream_t stream) {
   const bool few = (int64_t)a.max_tokens * a.group <= 16;
   int64_t keys = (int64_t)a.table_width * a.page_size;
   if (a.max_length < keys) keys = a.max_length;
@@ -229,13 +251,13 @@ void launch_weights(Attn4Args a, int d, hipStream_t stream) {
         a.chunk = (int)chunk;
         a.items = (int)(items * ((most + chunk - 1) / chunk));
         a.spread = 1;
-        constexpr uint32_t kLds = C::RING ? C::kWaves * Ring4<C, false>::kBytes : 0;
+        constexpr uint32_t kLds = ring_bytes<C, false>();
         static_assert(kLds <= 65536, "no attribute is asked for");
         hipLaunchKernelGGL(key_weights_few_kernel<C>, dim3((unsigned)a.items), dim3(C::kThreads), kLds, stream, a);
       };
       const int64_t pairs = (int64_t)a.N * a.kv_heads;
       if constexpr (RING) {
-        if (a.kv_heads % 4 == 0 && pairs * most >= LEAST_TILES)
+        if (a.kv_heads % 4 == 0 && heads_together && pairs * most >= LEAST_TILES)
           return launch(Attn4Config<T, D, 1, 4, 1, 1, RING>(), pairs / 4, CHUNK_TILES);
       }
       const int64_t want = 1024, fit = (most + 7) / 8;
@@ -269,8 +291,8 @@ lilicorr_status run_weights(const lilicorr_key_weights_args& x, hipStream_t stre
   a.lse_in = x.lse;
   a.weights = x.weights;
   a.decay = x.decay;
-  if (ring_fits(x.cache)) launch_weights<T, true>(a, a.d, stream);
-  else launch_weights<T, false>(a, a.d, stream);
+  if (ring_fits(x.cache)) launch_weights<T, true>(a, a.d, heads_together(x.cache), stream);
+  else launch_weights<T, false>(a, a.d, false, stream);
   return launch_status();
 }
 

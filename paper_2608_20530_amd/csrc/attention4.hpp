@@ -222,64 +222,22 @@ __device__ __forceinline__ X pick(bool first, X a, X b) {
   return first ? a : b;
 }
 
-template <typename C, bool VALUES>
-struct Ring4 {
-  static constexpr int D = C::D, RB = D / 2;      // bytes of a key's codes
-  static constexpr int CPR = D / 32;              // 16-byte pieces of them
-  static constexpr int KI = 32 * CPR / kWave;     // copies of a tile's keys, D = 64, 128, 256: 1, 2, 4
-  static constexpr int SB = D <= 128 ? 4 : 8;     // bytes of a key's scales, in LDS
-  static constexpr uint32_t kV = 32 * RB, kS = VALUES ? 2 * kV : kV;
-  static constexpr uint32_t kW = kS + 256;  // without values: the keys' weights
-  static constexpr uint32_t kStage = kS + (D <= 128 && VALUES ? 256 : 512);
-  static constexpr int IPS = KI * (VALUES ? 2 : 1) + (D <= 128 && VALUES ? 1 : 2);  // copies of a stage
-  static constexpr int NS = C::NS;
-    static constexpr uint32_t kBytes = NS * kStage;
-  static constexpr int kBatch = kWave / 2;        // tiles whose places the lanes have, a half each
-
-  const unsigned char *k, *v, *ks, *vs;
+// Where tiles lie. Offsets are bytes of codes from the head's first one on.
+template <bool VALUES>
+struct Where4 {
+  static constexpr int kBatch = kWave / 2;  // tiles whose places the lanes have, a half each
   const int32_t* trow;
-  lds_t lds;
-  uint32_t k_off[2], v_off[2];  // of a lane's piece: bytes
-  uint32_t s_off;
-  uint32_t k_at, k_x, v_at, ks_at, vs_at;  // LDS offsets of its reads
-  int e_last;                   // last entry that there is
-  int base;                     // first tile of the batch
-  uint64_t off;                 // of this lane's half: bytes of codes from the head's first
-  int64_t w;                    // and its first key's weight, without values
-  uint64_t valid;               // the halves whose page is there
-  uint32_t ahead;               // page of the next batch's half
-  uint64_t seen;                // two bits a tile that was found, the last one's lowest
+  int e_last;      // last entry that there is
+  int base;        // first tile of the batch
+  uint64_t off;    // of this lane's half
+  int64_t w;       // and its first key's weight, without values
+  uint64_t valid;  // the halves whose page is there
+  uint32_t ahead;  // page of the next batch's half
+  uint64_t seen;   // two bits a tile that was found, the last one's lowest
 
-  __device__ __forceinline__ void set(const Attn4Args& a, const unsigned char* k_, const unsigned char* v_,
-                                      const unsigned char* ks_, const unsigned char* vs_, const int32_t* trow_,
-                                      int keys, lds_t lds_) {
-    k = k_; v = v_; ks = ks_; vs = vs_; trow = trow_; lds = lds_;
-    const int lane = lane_id(), c = lane & 15, g = lane >> 4;
-    const uint32_t ts = (uint32_t)a.token_stride;
-    // LDS row r of a half has key r, piece x at place x ^ swizzle(r), or of values key 4 (r % 4) + r / 4 as it is
-    const int per = D == 64 ? 32 : kWave;  // lanes that a half's (or with 256 a quarter's) rows take
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      const int r = (lane % per) / CPR + (D == 256 ? 8 * y : 0), x = lane % CPR;
-      k_off[y] = r * ts + (x ^ swizzle(r)) * 16;
-      v_off[y] = (4 * (r % 4) + r / 4) * ts + x * 16;
-    }
-    s_off = (D <= 128 ? lane % 16 : lane / 2 % 16) * (ts / 16) + (D <= 128 ? 0 : lane % 2 * 4);
-    k_at = c * RB + (D == 64 ? (uint32_t)((g / 2 ^ swizzle(c)) * 16 + g % 2 * 8) : 0u);
-    k_x = swizzle(c);
-    v_at = kV + g * RB + c * C::VB;
-    ks_at = kS + c * SB + (D == 64 ? g / 2 : D == 128 ? g : 2 * g);
-    vs_at = kS + 32 * SB + 4 * g * SB + (D > 128 ? c / 2 : 0);
-    e_last = entry4(a, keys - 1);
-  }
-  static __device__ __forceinline__ uint32_t swizzle(int r) {
-    return D == 64 ? (r >> 3) & 1 : D == 128 ? (r >> 2) & 3 : (r >> 1) & 7;
-  }
-
-  // offsets (bytes of codes) of the two halves of a tile
-  struct At {
+  struct At {  // a tile's two halves
     uint64_t off0, off1;
-    int64_t w0, w1;       // without values
+    int64_t w0, w1;  // without values
   };
   // The s-th of `tiles` tiles, the number of which in the sequence tile_of gives; one after the other. 64 lanes work the
   // places of 32 tiles out at once, which costs a tile four v_readlane (a tile's places by scalar instructions
@@ -305,8 +263,11 @@ struct Ring4 {
   // before the first find(): everything that has been asked for so far is there afterwards, so that the compiler puts no
   // wait for it among the copies, which it does not see
   template <typename F>
-  __device__ __forceinline__ void begin(const Attn4Args& a, int tiles, const F& tile_of, int head = 0) {
+  __device__ __forceinline__ void begin(const Attn4Args& a, const int32_t* row, int keys, int tiles, const F& tile_of,
+                                        int head = 0) {
     int j;
+    trow = row;
+    e_last = entry4(a, keys - 1);
     ahead = (uint32_t)trow[entry_at(a, 0, tiles, tile_of, j)];
     seen = 0;
     batch(a, 0, tiles, tile_of, head);
@@ -332,7 +293,52 @@ struct Ring4 {
     const uint32_t b = (uint32_t)(seen >> (2 * back));
     return ((b & 1) ? 0xffffu : 0u) | ((b & 2) ? 0xffff0000u : 0u);
   }
-  __device__ __forceinline__ void copy(const Attn4Args& a, const At& at, int stage) const {
+};
+
+template <typename C, bool VALUES>
+struct Ring4 {
+  static constexpr int D = C::D, RB = D / 2;      // bytes of a key's codes
+  static constexpr int CPR = D / 32;              // 16-byte pieces of them
+  static constexpr int KI = 32 * CPR / kWave;     // copies of a tile's keys, D = 64, 128, 256: 1, 2, 4
+  static constexpr int SB = D <= 128 ? 4 : 8;     // bytes of a key's scales, in LDS
+  static constexpr uint32_t kV = 32 * RB, kS = VALUES ? 2 * kV : kV;
+  static constexpr uint32_t kW = kS + 256;  // without values: the keys' weights
+  static constexpr uint32_t kStage = kS + (D <= 128 && VALUES ? 256 : 512);
+  static constexpr int IPS = KI * (VALUES ? 2 : 1) + (D <= 128 && VALUES ? 1 : 2);  // copies of a stage
+  static constexpr int NS = C::NS;
+    static constexpr uint32_t kBytes = NS * kStage;
+
+  const unsigned char *k, *v, *ks, *vs;
+  lds_t lds;
+  uint32_t k_off[2], v_off[2];  // of a lane's piece: bytes
+  uint32_t s_off;
+  uint32_t k_at, k_x, v_at, ks_at, vs_at;  // LDS offsets of its reads
+
+  __device__ __forceinline__ void set(const Attn4Args& a, const unsigned char* k_, const unsigned char* v_,
+                                      const unsigned char* ks_, const unsigned char* vs_, lds_t lds_) {
+    k = k_; v = v_; ks = ks_; vs = vs_; lds = lds_;
+    const int lane = lane_id(), c = lane & 15, g = lane >> 4;
+    const uint32_t ts = (uint32_t)a.token_stride;
+    // LDS row r of a half has key r, piece x at place x ^ swizzle(r), or of values key 4 (r % 4) + r / 4 as it is
+    const int per = D == 64 ? 32 : kWave;  // lanes that a half's (or with 256 a quarter's) rows take
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int r = (lane % per) / CPR + (D == 256 ? 8 * y : 0), x = lane % CPR;
+      k_off[y] = r * ts + (x ^ swizzle(r)) * 16;
+      v_off[y] = (4 * (r % 4) + r / 4) * ts + x * 16;
+    }
+    s_off = (D <= 128 ? lane % 16 : lane / 2 % 16) * (ts / 16) + (D <= 128 ? 0 : lane % 2 * 4);
+    k_at = c * RB + (D == 64 ? (uint32_t)((g / 2 ^ swizzle(c)) * 16 + g % 2 * 8) : 0u);
+    k_x = swizzle(c);
+    v_at = kV + g * RB + c * C::VB;
+    ks_at = kS + c * SB + (D == 64 ? g / 2 : D == 128 ? g : 2 * g);
+    vs_at = kS + 32 * SB + 4 * g * SB + (D > 128 ? c / 2 : 0);
+  }
+  static __device__ __forceinline__ uint32_t swizzle(int r) {
+    return D == 64 ? (r >> 3) & 1 : D == 128 ? (r >> 2) & 3 : (r >> 1) & 7;
+  }
+
+  __device__ __forceinline__ void copy(const Attn4Args& a, const typename Where4<VALUES>::At& at, int stage) const {
     const lds_t to = lds + (uint32_t)stage * kStage;
     if constexpr (D == 64) {
       const uint64_t off = pick(lane_id() < 32, at.off0, at.off1);
@@ -410,6 +416,149 @@ struct Ring4 {
 #pragma unroll
           for (int e = 0; e < 4; ++e) r.vs[4 * h + e] = *(at + vs_at + (16 * h + e) * SB);
         }
+      }
+    }
+  }
+};
+
+// The ring of a workgroup whose waves go through the same keys: WH neighbouring key heads (side by side in every token) and
+// WR shares of the rows. Its waves share the copies, so that a copy takes whole lines: with a ring for each wave the same
+// line was asked for by two waves at once, for which the L1 waits (256 tokens 559 us, 547 with nothing but the
+// copies). Rows of WH heads lie in LDS as they do in the cache, keys in their order and values as in Ring4,
+// pieces permuted so that reads meet no bank conflicts.
+template <typename C, bool VALUES>
+struct Shared4 {
+  static constexpr int D = C::D, RB = D / 2, HB = C::WH, W = HB * RB;  // bytes of a token's codes
+  static constexpr int CPR = D / 32, P = W / 16;          // 16-byte pieces of a head, of a token
+  static constexpr int RPI = kWave / P;                   // tokens that a copy moves
+  static constexpr int KI = 32 / RPI;                     // copies of a tile's keys
+  static constexpr int SB = D == 64 && HB == 1 ? 4 : D / 32;  // bytes of a head's scales of a key, in LDS
+  static constexpr int SW = HB * SB;                      // and of the token's
+  static constexpr bool kBoth = 32 * SW <= 128;           // one copy has keys' scales and values'
+  static constexpr int SI = kBoth ? 1 : 32 * SW / 256;    // copies of the keys' scales
+  static constexpr uint32_t kV = 32 * W, kS = VALUES ? 2 * kV : kV, kVS = kBoth ? 128 : 32 * SW;
+  static constexpr uint32_t kW = kS + (kBoth ? 256 : 32 * SW);  // without values: the keys' weights, 256 bytes a head
+  static constexpr uint32_t kStage = VALUES ? kS + (kBoth ? 256 : 64 * SW) : kW + HB * 256;
+  static constexpr int kCodes = VALUES ? 2 * KI : KI, kAll = kCodes + (VALUES && !kBoth ? 2 * SI : SI);
+  static constexpr int CW = (kCodes + 3) / 4, SCW = (kAll - kCodes + 3) / 4;  // a wave's copies of codes, of scales
+  static constexpr int IPS = CW + SCW + (VALUES ? 0 : 1);
+  static constexpr int NS = C::NS;
+  static constexpr uint32_t kBytes = NS * kStage;
+  static_assert(C::kWaves == 4 && C::WK == 1, "four waves, the same keys");
+  static_assert(RPI <= 16 || RPI == 32, "a copy's tokens lie in one half, or are both");
+
+  const unsigned char *k, *v, *ks, *vs;  // of the workgroup's first head
+  lds_t lds;
+  int wave;
+  uint32_t c_off[CW];  // of the lane's piece in the wave's copies of codes, within the half: bytes
+  uint32_t s_off[SCW];
+  uint32_t k_at, k_x, k_p, v_at, ks_at, vs_at;
+
+  static __device__ __forceinline__ uint32_t swizzle(int r) { return W >= 256 ? r & 15 : (r / (256 / W)) & (P - 1); }
+  // (which copy a wave's i-th one is; those past the last are the last one again)
+  __device__ __forceinline__ int code_copy(int i) const { return min(wave + 4 * i, kCodes - 1); }
+  __device__ __forceinline__ int scale_copy(int i) const { return min(wave + 4 * i, kAll - kCodes - 1); }
+
+  __device__ __forceinline__ void set(const Attn4Args& a, const unsigned char* k_, const unsigned char* v_,
+                                      const unsigned char* ks_, const unsigned char* vs_, lds_t lds_, int wave_, int hh) {
+    k = k_; v = v_; ks = ks_; vs = vs_; lds = lds_; wave = wave_;
+    const int lane = lane_id(), c = lane & 15, g = lane >> 4;
+    const uint32_t ts = (uint32_t)a.token_stride;
+#pragma unroll
+    for (int i = 0; i < CW; ++i) {
+      const int n = code_copy(i);
+      const int r = (n % KI * RPI + lane / P) % 16, x = lane % P;
+      c_off[i] = n < KI ? r * ts + (x ^ swizzle(n % KI * RPI + lane / P)) * 16
+                        : (4 * (r % 4) + r / 4) * ts + (x ^ (uint32_t)(CPR * ((r & 3) * HB / 4))) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < SCW; ++i) {
+      // dword `at` of the tile's keys' (or values') scales
+      const int at = kBoth ? lane % 32 : (scale_copy(i) % SI) * 64 + lane, key = at * 4 / SW;
+      s_off[i] = key % 16 * (ts / 16) + at * 4 % SW;
+    }
+    k_at = c * W;
+    k_x = swizzle(c);
+    k_p = hh * CPR;
+    // (the lane's keys have R = 4 e + g: the permutation depends on g alone)
+    const uint32_t piece = (uint32_t)(hh * CPR + c * C::VB / 16) ^ (uint32_t)(CPR * (g * HB / 4));
+    v_at = kV + g * W + piece * 16 + c * C::VB % 16;
+    ks_at = kS + c * SW + hh * SB + (D == 64 ? g / 2 : D == 128 ? g : 2 * g);
+    vs_at = kS + kVS + 4 * g * SW + hh * SB + c / (512 / D);
+  }
+  __device__ __forceinline__ void copy(const Attn4Args& a, const typename Where4<VALUES>::At& at, int stage, int hh) const {
+    const lds_t to = lds + (uint32_t)stage * kStage;
+#pragma unroll
+    for (int i = 0; i < CW; ++i) {
+      const int n = code_copy(i);
+      const bool is_k = n < KI;
+      const unsigned char* from = pick(is_k, k, v);
+      const lds_t dst = to + n * 1024;
+      if constexpr (RPI == 32) {
+        copy16(dst, from + pick(lane_id() < 32, at.off0, at.off1) + c_off[i]);
+      } else {
+        copy16(dst, from + pick(n % KI < KI / 2, at.off0, at.off1), c_off[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < SCW; ++i) {
+      const int n = scale_copy(i);
+      const lds_t dst = to + kS + n * 256;
+      if constexpr (kBoth) {
+        const int key = lane_id() % 32 * 4 / SW;
+        copy4<D == 64 && HB == 1>(dst, pick(VALUES && lane_id() >= 32, vs, ks) + pick(key < 16, at.off0, at.off1) / 16 + s_off[i]);
+      } else {
+        const int key = ((n % SI) * 64 + lane_id()) * 4 / SW;
+        copy4<false>(dst, pick(n < SI, ks, vs) + pick(key < 16, at.off0, at.off1) / 16 + s_off[i]);
+      }
+    }
+    if constexpr (!VALUES)  // each wave its own head's weights
+      copy4<false>(to + kW + hh * 256,
+                   (const unsigned char*)(a.weights + pick((lane_id() & 16) == 0, at.w0, at.w1) + lane_id() % 16));
+  }
+  __device__ __forceinline__ void read(int stage, Raw4<C>& r) const {
+    typedef __attribute__((address_space(3))) uint16_t* lds_u16_t;
+    typedef __attribute__((address_space(3))) u32x2_t* lds_u32x2_t;
+    const lds_t at = lds + (uint32_t)stage * kStage;
+    const int g = lane_id() >> 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // (keys 16 apart differ in the permutation where a half is not a whole number of its turns)
+      const uint32_t x = k_x ^ (h ? swizzle(16) : 0);
+      if constexpr (D == 64) {
+        const u32x2_t w = *(lds_u32x2_t)(at + h * 16 * W + k_at + ((k_p + g / 2) ^ x) * 16 + g % 2 * 8);
+        r.k[h][0] = w[0];
+        r.k[h][1] = w[1];
+      } else {
+#pragma unroll
+        for (int y = 0; y < C::KW / 4; ++y) {
+          const u32x4_t w = *(lds_u32x4_t)(at + h * 16 * W + k_at + ((k_p + g * (C::KW / 4) + y) ^ x) * 16);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r.k[h][4 * y + i] = w[i];
+        }
+      }
+      if constexpr (C::KS > 1) {
+        const uint32_t w = *(lds_u16_t)(at + ks_at + h * 16 * SW);
+        r.ks[h][0] = w & 0xff;
+        r.ks[h][1] = w >> 8;
+      } else {
+        r.ks[h][0] = *(at + ks_at + h * 16 * SW);
+      }
+    }
+    if constexpr (VALUES) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const lds_t from = at + v_at + ((e / 4) * 16 + (e % 4) * 4) * W;
+        if constexpr (C::VB == 2) {
+          r.v[e][0] = *(lds_u16_t)from;
+        } else if constexpr (C::VB == 4) {
+          r.v[e][0] = *(lds_u32_t)from;
+        } else {
+          const u32x2_t w = *(lds_u32x2_t)from;
+          r.v[e][0] = w[0];
+          r.v[e][1] = w[1];
+        }
+        r.vs[e] = *(at + vs_at + ((e / 4) * 16 + e % 4) * SW);
       }
     }
   }
@@ -725,33 +874,61 @@ void attention4_kernel(Attn4Args a) {
   };
   int i = t_begin + wk;
   if constexpr (C::RING) {
-    Ring4<C, true> ring;
+    constexpr bool kShared = C::WK == 1;
+    typedef std::conditional_t<kShared, Shared4<C, true>, Ring4<C, true>> Ring;
+    Ring ring;
+    Where4<true> where;
     if (i < t_end) {
-      ring.set(a, k, v, ks, vs, trow, hi, (lds_t)attn4_smem + (uint32_t)wave * Ring4<C, true>::kBytes);
-      const int tiles = (t_end - i + C::WK - 1) / C::WK;  // of this wave; NS of them are under way
-      auto tile_of = [&](int s) { return tile_at(i + s * C::WK); };
-      auto find = [&](int s) { return ring.find(a, s, tiles, tile_of); };
-      ring.begin(a, tiles, tile_of);
-#pragma unroll
-      for (int s = 0; s < C::NS; ++s) {
-        const auto first = find(s);
-        if (s < tiles) ring.copy(a, first, s);
+      if constexpr (kShared) {
+        const int64_t first = (int64_t)(head - wh) * a.head_stride;
+        ring.set(a, a.k + first, a.v + first, a.ks + first / 16, a.vs + first / 16, (lds_t)attn4_smem, wave, wh);
+      } else {
+        ring.set(a, k, v, ks, vs, (lds_t)attn4_smem + (uint32_t)wave * Ring::kBytes);
       }
-      auto next = find(C::NS);
+      const int tiles = (t_end - i + C::WK - 1) / C::WK;  // of this wave
+      auto tile_of = [&](int s) { return tile_at(i + s * C::WK); };
+      auto find = [&](int s) { return where.find(a, s, tiles, tile_of); };
+      auto copy = [&](const typename Where4<true>::At& from, int stage) __attribute__((always_inline)) {
+        if constexpr (kShared) ring.copy(a, from, stage, wh);
+        else ring.copy(a, from, stage);
+      };
+      // A wave with a ring of its own has NS tiles under way, and copies the next one when it is done with one. Shared, NS - 1:
+      // the barrier says that everyone's copies have landed, and that all are done with the tile before, whose place
+      // the next copies take.
+      constexpr int kAhead = kShared ? C::NS - 1 : C::NS;
+      where.begin(a, trow, hi, tiles, tile_of);
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        const auto first = find(s);
+        if (s < tiles) copy(first, s);
+      }
+      auto next = find(kAhead);
       int at = 0, s = 0;
+      bool begun = false;  // this tile has been waited for
       while (true) {
         for (; s < tiles; ++s) {
-          if (s + C::NS - 1 < tiles)
-            __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NS - 1) * Ring4<C, true>::IPS) : "memory");
-          else
-            __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          if (!begun) {
+            if (s + kAhead - 1 < tiles)
+              __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"((kAhead - 1) * Ring::IPS) : "memory");
+            else
+              __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if constexpr (kShared) {
+              __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+              if (s + kAhead < tiles) copy(next, at == 0 ? C::NS - 1 : at - 1);
+              next = find(s + kAhead + 1);
+            }
+          }
           Raw4<C> r;
           ring.read(at, r);
           const int x = i + s * C::WK;
-          if (!use(r, x, ring.there(C::NS))) break;
-          __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this stage's reads, whose place is copied to next
-          if (s + C::NS < tiles) ring.copy(a, next, at);
-          next = find(s + C::NS + 1);
+          begun = true;
+          if (!use(r, x, where.there(kShared ? kAhead + 1 : kAhead))) break;
+          begun = false;
+          if constexpr (!kShared) {
+            __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this tile's reads
+            if (s + kAhead < tiles) copy(next, at);
+            next = find(s + kAhead + 1);
+          }
           at = at + 1 == C::NS ? 0 : at + 1;
         }
         if (s >= tiles) break;
@@ -1021,33 +1198,51 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args 
     return a.weights[weight_at(a, place(page), head, min(x, t_end - 1) * 32 + (lane & 31))];
   };
   if constexpr (C::RING) {
-    typedef Ring4<C, false> Ring;
+    constexpr bool kShared = C::WK == 1;
+    typedef std::conditional_t<kShared, Shared4<C, false>, Ring4<C, false>> Ring;
+    typedef Where4<false> Where;
     Ring ring;
-    ring.set(a, k, k, ks, ks, trow, hi, (lds_t)attn4_smem + (uint32_t)wave * Ring::kBytes);
+    Where places;
+    if constexpr (kShared) {
+      const int64_t first = (int64_t)(head - wh) * a.head_stride;
+      ring.set(a, a.k + first, a.k, a.ks + first / 16, a.ks, (lds_t)attn4_smem, wave, wh);
+    } else {
+      ring.set(a, k, k, ks, ks, (lds_t)attn4_smem + (uint32_t)wave * Ring::kBytes);
+    }
     const int tiles = (t_end - i + C::WK - 1) / C::WK;
     auto tile_of = [&](int s) { return i + s * C::WK; };
-    auto find = [&](int s) { return ring.find(a, s, tiles, tile_of, head); };
-    ring.begin(a, tiles, tile_of, head);
-    typename Ring::At where[C::NS + 1];  // of the tiles under way, this one first
+    auto find = [&](int s) { return places.find(a, s, tiles, tile_of, head); };
+    auto copy = [&](const typename Where::At& from, int stage) __attribute__((always_inline)) {
+      if constexpr (kShared) ring.copy(a, from, stage, wh);
+      else ring.copy(a, from, stage);
+    };
+    places.begin(a, trow, hi, tiles, tile_of, head);
+    typename Where::At where[C::NS + 1];  // of the tiles under way, this one first
 #pragma unroll
     for (int s = 0; s <= C::NS - 1; ++s) {
       where[s] = find(s);
-      if (s < C::NS - 1 && s < tiles) ring.copy(a, where[s], s);
+      if (s < C::NS - 1 && s < tiles) copy(where[s], s);
     }
     int at = 0, to = C::NS - 1;
+    constexpr int kAhead = kShared ? C::NS - 2 : C::NS - 1;  // tiles under way while this one is waited for
     for (int s = 0; s < tiles; ++s) {
       __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (s + C::NS - 1 < tiles) {
-        ring.copy(a, where[C::NS - 1], to);
-        __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NS - 1) * Ring::IPS) : "memory");
-      } else {
+      if constexpr (!kShared) {
+        if (s + C::NS - 1 < tiles) copy(where[C::NS - 1], to);
+      }
+      if (s + kAhead < tiles)
+        __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead * Ring::IPS) : "memory");
+      else
         __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if constexpr (kShared) {
+        __asm__ volatile("s_barrier" ::: "memory");
+        if (s + C::NS - 1 < tiles) copy(where[C::NS - 1], to);
       }
       Raw4<C> r;
       ring.read(at, r);
-      const float before = *(lds_float_t)(ring.lds + (uint32_t)at * Ring::kStage + Ring::kW + (lane & 31) * 4);
+      const float before = *(lds_float_t)(ring.lds + (uint32_t)at * Ring::kStage + Ring::kW + (kShared ? wh * 256 : 0) + (lane & 31) * 4);
       where[C::NS] = find(s + C::NS);
-      const uint32_t there = ring.there(C::NS);
+      const uint32_t there = places.there(C::NS);
       const int x = i + s * C::WK;
       const float w = use(r, before, x);
       if (lane < 32 && x * 32 + lane < hi && (there >> lane & 1))
