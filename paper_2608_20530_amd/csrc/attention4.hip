@@ -11,13 +11,9 @@
 
 namespace lilicorr {
 namespace {
-#ifndef LEAST_TILES
-#define LEAST_TILES 65536
-#endif
-#ifndef CHUNK_TILES
-#define CHUNK_TILES 64
-#endif
 
+// Many keys in all: a workgroup's waves share key heads rather than keys
+constexpr int64_t kManyTiles = 65536;
 constexpr size_t kLeastBytes4 = 256;  // of a workspace
 // The longest sequences have so many tokens: lengths, windows and sinks past it say "without end"
 constexpr int64_t kMost4 = (int64_t)1 << 30;
@@ -40,11 +36,7 @@ void with_rows4(int BM, bool heads, const F& use) {
       if (BM == 16) return use(Attn4Config<T, D, 1, 4, 1, 1, RING>());
       if constexpr (D <= 128) {
         if (BM == 32) return use(Attn4Config<T, D, 2, 4, 1, 1, RING>());
-#ifdef B64
-        if (BM == 64) return use(Attn4Config<T, D, 4, 4, 1, 1, RING>());
-#else
         if (BM == 64) return use(Attn4Config<T, D, 2, 2, 2, 1, RING>());
-#endif
       } else {
         if (BM == 32) return use(Attn4Config<T, D, 1, 2, 2, 1, RING>());
       }
@@ -130,27 +122,25 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
   p.ring = ring_fits(a.cache);
   p.spread = own <= p.BM;
   // key heads over the waves, where that still leaves every compute unit work
-#ifdef B64
-  const int most_rows = 64;
-#else
-  const int most_rows = 32;
-#endif
-  const int wide = p.BM <= 16 || (p.BM <= most_rows && a.cache.d <= 128) ? 4 : p.BM <= 64 && (a.cache.d <= 128 || p.BM == 32) ? 2 : 1;
+  const int wide = p.BM <= 16 || (p.BM <= 32 && a.cache.d <= 128) ? 4 : p.BM <= 64 && (a.cache.d <= 128 || p.BM == 32) ? 2 : 1;
   const int64_t pairs = tiles * a.cache.heads;
-  p.heads = p.ring && wide > 1 && a.cache.heads % wide == 0 && heads_together(a.cache) && pairs * most >= LEAST_TILES ? wide : 1;
+  p.heads = p.ring && wide > 1 && a.cache.heads % wide == 0 && heads_together(a.cache) && pairs * most >= kManyTiles ? wide : 1;
   const int64_t items = pairs / p.heads, wk = p.heads > 1 ? 1 : p.BM <= 32 ? (p.BM == 32 && a.cache.d > 128 ? 2 : 4) : p.BM == 64 && a.cache.d <= 128 ? 2 : 1;
   int64_t chunk, chunks;
   if (p.heads > 1) {
-    chunk = CHUNK_TILES;
+    // A workgroup's share of the time should be small, the partial results' too, which with more rows weigh more: 256 tokens
+    // 466 us with 64 tiles a chunk, 474 with 48, 494 with 84; 64 blocks 379 with 84, 407 with 64, 385 with 128
+    chunk = (most * items + 1535) / 1536;
+    const int64_t cap = p.BM <= 16 ? 64 : 84;
+    chunk = chunk < 8 ? 8 : chunk > cap ? cap : chunk;
     chunks = (most + chunk - 1) / chunk;
-    if (chunks > 64) chunks = 64;
   } else {
     const int64_t want = 768;
     chunks = items >= want ? 1 : want / items;
     const int64_t fit = (most + 2 * wk - 1) / (2 * wk);
     if (chunks > fit) chunks = fit;
-    if (chunks > 64) chunks = 64;
   }
+  if (chunks > 64) chunks = 64;
   chunk = (most + chunks - 1) / chunks;
   chunks = (most + chunk - 1) / chunk;
   if (tiles * chunks > 0x7fffffffll / a.cache.heads) return LILICORR_ERR_UNSUPPORTED;
@@ -175,6 +165,7 @@ Attn4Args common4(const A& x) {
   a.rows = x.tokens * x.heads;
   a.N = (int)x.N; a.pages = (int)c.pages; a.page_size = (uint32_t)c.page_size; a.table_width = (int)x.table_width;
   divide_by(c.page_size, a.page_mul, a.page_shift);
+  divide_by(x.heads / c.heads, a.group_mul, a.group_shift);
   a.tokens = (int)x.tokens; a.heads = x.heads; a.kv_heads = c.heads; a.group = x.heads / c.heads; a.d = c.d;
   a.max_tokens = (int)(x.max_tokens < x.tokens ? x.max_tokens : x.tokens);
   a.max_length = (int)bounded4(x.max_length);
@@ -187,7 +178,7 @@ Attn4Args common4(const A& x) {
 template <typename C, bool VALUES>
 constexpr uint32_t ring_bytes() {
   if constexpr (!C::RING) return 0;
-  else if constexpr (C::WK == 1) return Shared4<C, VALUES>::kBytes;
+  else if constexpr (C::kShared) return Shared4<C, VALUES>::kBytes;
   else return C::kWaves * Ring4<C, VALUES>::kBytes;
 }
 
@@ -208,8 +199,11 @@ void launch4(const Attn4Args& a, hipStream_t stream) {
 template <typename T, int LPR>
 void launch_join4(const Attn4Args& a, int slots, hipStream_t stream) {
   constexpr int64_t per = kJoin4Threads / kWave;
-  hipLaunchKernelGGL((attention4_join_kernel<T, LPR>), dim3((unsigned)((a.rows + per - 1) / per)), dim3(kJoin4Threads), 0,
-                     stream, a, slots);
+  const dim3 grid((unsigned)((a.rows + per - 1) / per));
+  if (a.rows <= 1024)
+    hipLaunchKernelGGL((attention4_join_kernel<T, LPR, true>), grid, dim3(kJoin4Threads), 0, stream, a, slots);
+  else
+    hipLaunchKernelGGL((attention4_join_kernel<T, LPR, false>), grid, dim3(kJoin4Threads), 0, stream, a, slots);
 }
 
 template <typename T>
@@ -234,7 +228,19 @@ lilicorr_status run4(const lilicorr_attention4_args& x, const Plan4& p, hipStrea
   return launch_status();
 }
 
-// keys of a tile of key_weights_many_kernel: WK waves of 64
+template <typename C>
+void launch_many(const Attn4Args& a, hipStream_t stream) {
+  constexpr uint32_t kLds = Rows4Ring<C>::kBytes;
+  if constexpr (kLds > 65536) {
+    static const hipError_t attr =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(key_weights_many_kernel<C>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+    (void)attr;
+  }
+  hipLaunchKernelGGL(key_weights_many_kernel<C>, dim3((unsigned)((int64_t)a.tiles * a.N * a.kv_heads)),
+                     dim3(C::kThreads), kLds, stream, a);
+}
+
 template <typename T, bool RING>
 void launch_weights(Attn4Args a, int d, bool heads_together, hipStream_t stream) {
   const bool few = (int64_t)a.max_tokens * a.group <= 16;
@@ -257,8 +263,9 @@ void launch_weights(Attn4Args a, int d, bool heads_together, hipStream_t stream)
       };
       const int64_t pairs = (int64_t)a.N * a.kv_heads;
       if constexpr (RING) {
-        if (a.kv_heads % 4 == 0 && heads_together && pairs * most >= LEAST_TILES)
-          return launch(Attn4Config<T, D, 1, 4, 1, 1, RING>(), pairs / 4, CHUNK_TILES);
+        // (nothing is joined, so chunks are short: 256 tokens 283 us with 16 tiles, 290 with 32, 305 with 64)
+        if (a.kv_heads % 4 == 0 && heads_together && pairs * most >= kManyTiles)
+          return launch(Attn4Config<T, D, 1, 4, 1, 1, RING>(), pairs / 4, 16);
       }
       const int64_t want = 1024, fit = (most + 7) / 8;
       int64_t chunks = pairs >= want ? 1 : want / pairs;
@@ -270,13 +277,11 @@ void launch_weights(Attn4Args a, int d, bool heads_together, hipStream_t stream)
       if (groups * a.N * a.kv_heads >= 2048) {
         typedef Attn4Config<T, D, 1, 1, 1, 4, false> C;
         a.tiles = (int)((groups + 3) / 4);
-        hipLaunchKernelGGL(key_weights_many_kernel<C>, dim3((unsigned)((int64_t)a.tiles * a.N * a.kv_heads)),
-                           dim3(C::kThreads), 0, stream, a);
+        launch_many<C>(a, stream);
       } else {
         typedef Attn4Config<T, D, 1, 1, 4, 1, false> C;
         a.tiles = (int)groups;
-        hipLaunchKernelGGL(key_weights_many_kernel<C>, dim3((unsigned)((int64_t)a.tiles * a.N * a.kv_heads)),
-                           dim3(C::kThreads), 0, stream, a);
+        launch_many<C>(a, stream);
       }
     }
   };

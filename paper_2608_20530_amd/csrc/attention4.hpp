@@ -58,6 +58,7 @@ struct Attn4Args {
   int64_t q_stride, rows;  // rows = tokens * heads
   int64_t head_stride;     // bytes
   int N, pages, table_width;
+  uint32_t group_mul, group_shift;           // n / group, likewise
   uint32_t page_mul, page_shift, page_size;  // n / page_size = (n * page_mul) >> page_shift
   int tokens, heads, kv_heads, group, d;
   int64_t page_stride, token_stride;  // bytes
@@ -78,14 +79,12 @@ struct Attn4Config {
   static constexpr int RT = RT_;  // blocks of 16 rows of a wave
   static constexpr int WH = WH_, WR = WR_, WK = WK_;  // waves of key heads by waves of rows by waves of keys
   static constexpr bool RING = RING_;  // tiles by way of LDS
-#ifndef SIMD1
-#define SIMD1 3
-#endif
-#ifndef NS1
-#define NS1 3
-#define NS4 4
-#endif
-  static constexpr int NS = RT == 4 ? (D <= 64 ? 10 : NS4) : D <= 64 ? 4 : D <= 128 ? NS1 : 2;  // stages of a wave's ring
+  // Several key heads in a workgroup: one ring for all. Rows of one head (prefill) do better each with their own copies than
+  // with a barrier a tile: 1966 us against 2095.
+  static constexpr bool kShared = WK == 1 && WH > 1;
+  // Stages of a ring. Two are enough where a compute unit has three workgroups (16 rows: 468 us for 256 tokens, 478 with
+  // three, 475 with four).
+  static constexpr int NS = D <= 64 ? 4 : D <= 128 && RT > 1 ? 3 : 2;
   static constexpr int kWaves = WH * WR * WK, kThreads = kWaves * kWave;
   static constexpr int BM = 16 * RT * WR;
   static constexpr int ND = D / 16;  // output products
@@ -99,7 +98,7 @@ struct Attn4Config {
   // waves of a SIMD that the registers are given out for: two or more keep the accumulators where the vector unit
   // reaches them
   static constexpr int kSimdWaves =
-      D > 128 || RT == 4 || (RT == 2 && D > 64 && kTerms > 1) ? 1 : RT == 1 && kTerms == 1 ? SIMD1 : 2;
+      D > 128 || (RT == 2 && D > 64 && kTerms > 1) ? 1 : RT == 1 && kTerms == 1 ? 3 : 2;
 };
 
 // What a wave has under way of a tile of 32 keys
@@ -874,7 +873,7 @@ void attention4_kernel(Attn4Args a) {
   };
   int i = t_begin + wk;
   if constexpr (C::RING) {
-    constexpr bool kShared = C::WK == 1;
+    constexpr bool kShared = C::kShared;
     typedef std::conditional_t<kShared, Shared4<C, true>, Ring4<C, true>> Ring;
     Ring ring;
     Where4<true> where;
@@ -1057,9 +1056,10 @@ void attention4_kernel(Attn4Args a) {
 }
 
 // Joins the slots of every row in their order, a wave a row: maxima and sums one lane a slot, then the partial outputs
-// in 16 bytes a lane, LPR lanes a slot and 64 / LPR slots at once.
+// in 16 bytes a lane, LPR lanes a slot and 64 / LPR slots at once. A slot that saw nothing holds no output. FEW rows:
+// all slots are read at once, beside the sums and without them; else only those that count.
 constexpr int kJoin4Threads = 256;
-template <typename T, int LPR>
+template <typename T, int LPR, bool FEW>
 __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Args a, int slots) {
   constexpr int kAtOnce = kWave / LPR;
   const int lane = lane_id();
@@ -1071,21 +1071,20 @@ __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Arg
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < slots; s0 += kWave) {
     const int here = min(slots - s0, kWave);
-    constexpr int kBatch = 8;
+    constexpr int kBatch = FEW ? 64 / kAtOnce : 8;
     f32x4_t v[kBatch];
-    // a slot that saw nothing holds no output: read all the same, beside its sum, and not used
-    auto load = [&](int b) {
+    auto load = [&](int b, uint64_t which) {
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         const int s = b + u * kAtOnce + lane / LPR;
         v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (s < here && x < a.d)
+        if (s < here && x < a.d && (FEW || (which >> (s & 63) & 1)))
           v[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + ((s0 + s) * a.rows + row) * a.d + x);
       }
     };
     f32x4_t ml = {-__builtin_inff(), 0.f, 0.f, 0.f};
     if (lane < here) ml = a.part_ml[(s0 + lane) * a.rows + row];
-    load(0);
+    if constexpr (FEW) load(0, 0);
     const float grown = fmaxf(top, wave_max_dpp(ml[0]));
     const float f0 = top == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(top - grown);
     // the sum of a slot that saw nothing is 0; a NaN stays one
@@ -1097,7 +1096,7 @@ __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Arg
     o *= f0;
     const uint64_t which = __ballot(saw);
     for (int b = 0; b < here; b += kBatch * kAtOnce) {
-      if (b) load(b);
+      if (!FEW || b) load(b, which);
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         const int s = b + u * kAtOnce + lane / LPR;
@@ -1198,7 +1197,7 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args 
     return a.weights[weight_at(a, place(page), head, min(x, t_end - 1) * 32 + (lane & 31))];
   };
   if constexpr (C::RING) {
-    constexpr bool kShared = C::WK == 1;
+    constexpr bool kShared = C::kShared;
     typedef std::conditional_t<kShared, Shared4<C, false>, Ring4<C, false>> Ring;
     typedef Where4<false> Where;
     Ring ring;
@@ -1286,10 +1285,26 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args 
 
 // More rows: a wave keeps 64 keys as operands and goes through the rows that see them, 16 at a time; the
 // scores stand as in the attention, S^T[key][row], so that a row's logarithm is one register and the sum over rows waits for
-// the end. The workgroup's waves have the keys of WK neighbouring groups and WR shares of the rows.
+// the end. The workgroup's waves have the keys of WK neighbouring groups and WR shares of the rows. Rows and their
+// logarithms come 64 at a time by way of LDS: loads in the operands' layout have neighbouring lanes in different rows
+// and kept the address unit busy four times as long as the matrix cores (a prompt's last 1024 tokens 525 us).
+__device__ const uint32_t kZeros4[4] = {0, 0, 0, 0};  // what is copied past the width of the head
+
+template <typename C>
+struct Rows4Ring {
+  static constexpr int kRows = 64, RB = C::D * 2, P = RB / 16;  // bytes of a row, 16-byte pieces
+  static constexpr int RPI = kWave / P, CW = 16 / RPI;          // rows that a copy moves, a wave's copies
+  static constexpr int NS = C::D <= 128 ? 3 : 2;
+  static constexpr uint32_t kLse = kRows * RB, kStage = kLse + 4 * 256, kBytes = NS * kStage;
+  static constexpr int IPS = CW + 1;
+  static __device__ __forceinline__ int swizzle(int r) { return RB >= 256 ? r & 15 : (r >> 1) & (P - 1); }
+};
+
 template <typename C>
 __global__ __launch_bounds__(C::kThreads) void key_weights_many_kernel(Attn4Args a) {
-  __shared__ float s_sum[C::kWaves][kWave];
+  extern __shared__ __attribute__((aligned(16))) unsigned char attn4_smem[];
+  typedef Rows4Ring<C> Ring;
+  static_assert(C::kWaves == 4, "four waves copy 16 rows each");
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = (int)uniform32(tid >> 6), wr = wave % C::WR, wk = wave / C::WR;
   const int head = (int)blockIdx.x % a.kv_heads;
@@ -1298,68 +1313,89 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_many_kernel(Attn4Args
   auto starts_at = [&](int i) { return min(max(a.starts[i], 0), a.tokens); };
   const int start = starts_at(n), T = starts_at(n + 1) - start, total = max(a.totals[n], 0), pos0 = total - T;
   const int hi = max((int)min((int64_t)min(total, a.max_length), a.table_width * (int64_t)a.page_size), 0);
-  const int j0 = ((rest % a.tiles) * C::WK + wk) * 64;
-  const bool any = T > 0 && T <= a.max_tokens && j0 < hi;
+  const int jg = (rest % a.tiles) * C::WK * 64;  // the workgroup's first key, and the wave's
+  const int j0 = jg + wk * 64;
+  if (T <= 0 || T > a.max_tokens || jg >= hi) return;
   float acc[4][4];
 #pragma unroll
   for (int h = 0; h < 4; ++h)
 #pragma unroll
     for (int r = 0; r < 4; ++r) acc[h][r] = 0.f;
   const int j = j0 + 16 * (c >> 2) + 4 * g + (c & 3);  // the key whose weight this lane writes
-  int my_page = -1;
-  if (any) {
-    const int32_t* trow = a.table + (int64_t)n * a.table_width;
-    u32x4_t kk[4][C::KW];
-    {
-      Places4<C> pl;
-      pl.set(a);
-      const int64_t ho = (int64_t)head * a.head_stride;
-      const unsigned char *k = a.k + ho, *ks = a.ks + ho / 16;
-      Raw4<C> r[2];
+  const int32_t* trow = a.table + (int64_t)n * a.table_width;
+  u32x4_t kk[4][C::KW];
+  {
+    Places4<C> pl;
+    pl.set(a);
+    const int64_t ho = (int64_t)head * a.head_stride;
+    const unsigned char *k = a.k + ho, *ks = a.ks + ho / 16;
+    Raw4<C> r[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int key = min(j0 + 32 * x + (lane & 31), hi - 1);
-        const int page = trow[entry4(a, key)];
-        load4<C, false>(a, pl, k, k, ks, ks, min(j0 / 32 + x, (hi - 1) / 32), page >= 0 && page < a.pages ? page : 0, r[x]);
-      }
-      if (j < hi) my_page = trow[entry4(a, j)];
-#pragma unroll
-      for (int h = 0; h < 4; ++h) keys4<C>(r[h >> 1], h & 1, kk[h]);
+    for (int x = 0; x < 2; ++x) {
+      const int key = min(j0 + 32 * x + (lane & 31), hi - 1);
+      const int page = trow[entry4(a, key)];
+      load4<C, false>(a, pl, k, k, ks, ks, min(j0 / 32 + x, (hi - 1) / 32), page >= 0 && page < a.pages ? page : 0, r[x]);
     }
-    const int rows = T * a.group;
-    const int first = a.causal ? max(j0 - pos0, 0) * a.group / 16 * 16 : 0;  // of the rows that see the first key
-    u32x4_t qa[C::KW], qb[C::KW];
-    float la, lb;
-    int ta, tb;
-    auto load = [&](int r0, u32x4_t (&q)[C::KW], float& ls, int& tok) __attribute__((always_inline)) {
-      const int r = r0 + c, rc = min(r, rows - 1);
-      tok = rc / a.group;
-      const int hq = head * a.group + (rc - tok * a.group);
-      const uint16_t* at = a.q + ((int64_t)start + tok) * a.q_stride + (int64_t)hq * a.d;
 #pragma unroll
-      for (int w = 0; w < C::KW; ++w) {
-        const int x = g * (C::D / 4) + w * 8;
-        q[w] = x < a.d ? *reinterpret_cast<const u32x4_t*>(at + x) : u32x4_t{0, 0, 0, 0};
-      }
-      ls = a.lse_in[((int64_t)start + tok) * a.heads + hq];
-      if (r >= rows) ls = -__builtin_inff();
-    };
-    auto use = [&](const u32x4_t (&in)[C::KW], float v, int tok) __attribute__((always_inline)) {
-      // no row, or one that sees nothing: its powers are 0
-      const bool none = v == -__builtin_inff();
-      const float ls = v * 1.4426950408889634f;
-      const int p = pos0 + tok;
-      const bool all = !__ballot(none || (a.causal && p < j0 + 63));
+    for (int h = 0; h < 4; ++h) keys4<C>(r[h >> 1], h & 1, kk[h]);
+  }
+  const int my_page = j < hi ? trow[entry4(a, j)] : -1;
+  const int rows = T * a.group;
+  // the first row that sees the workgroup's first key
+  const int first = a.causal ? max(jg - pos0, 0) * a.group / 64 * 64 : 0;
+  const int stages = rows > first ? (rows - first + 63) / 64 : 0;
+  auto token_of = [&](int row) { return (int)(((uint64_t)(uint32_t)row * a.group_mul) >> a.group_shift); };
+  auto copy = [&](int s) __attribute__((always_inline)) {
+    const lds_t to = (lds_t)attn4_smem + (uint32_t)(s % Ring::NS) * Ring::kStage;
+    const uint16_t* q = a.q + (int64_t)start * a.q_stride + (int64_t)head * a.group * a.d;
+#pragma unroll
+    for (int i = 0; i < Ring::CW; ++i) {
+      const int r = wave * 16 + i * Ring::RPI + lane / Ring::P;
+      const int piece = (lane % Ring::P) ^ Ring::swizzle(r), row = min(first + s * 64 + r, rows - 1), tok = token_of(row);
+      const uint16_t* at = q + (int64_t)tok * a.q_stride + (int64_t)(row - tok * a.group) * a.d + piece * 8;
+      copy16(to + (wave * 16 + i * Ring::RPI) * Ring::RB,
+             (const unsigned char*)(piece * 8 < a.d ? at : (const uint16_t*)kZeros4));
+    }
+    const int row = min(first + s * 64 + wave * 16 + c, rows - 1), tok = token_of(row);
+    copy4<false>(to + Ring::kLse + wave * 256,
+                 (const unsigned char*)(a.lse_in + ((int64_t)start + tok) * a.heads + head * a.group + (row - tok * a.group)));
+  };
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // the compiler's own loads, so that it waits for none among the copies
+#pragma unroll
+  for (int s = 0; s < Ring::NS - 1; ++s)
+    if (s < stages) copy(s);
+  for (int s = 0; s < stages; ++s) {
+    constexpr int kAhead = Ring::NS - 2;
+    if (s + kAhead < stages)
+      __asm__ volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead * Ring::IPS) : "memory");
+    else
+      __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (s + Ring::NS - 1 < stages) copy(s + Ring::NS - 1);
+    const lds_t from = (lds_t)attn4_smem + (uint32_t)(s % Ring::NS) * Ring::kStage;
+#pragma unroll 1
+    for (int u = wr; u < 4; u += C::WR) {
+      const int row = first + s * 64 + u * 16 + c;
+      if (first + s * 64 + u * 16 >= rows) break;
       u32x4_t q[C::KW][C::kTerms];
 #pragma unroll
-      for (int w = 0; w < C::KW; ++w) Query<typename C::T>::split(in[w], q[w]);
+      for (int w = 0; w < C::KW; ++w) {
+        const u32x4_t in = *(lds_u32x4_t)(from + (u * 16 + c) * Ring::RB + ((g * C::KW + w) ^ Ring::swizzle(u * 16 + c)) * 16);
+        Query<typename C::T>::split(in, q[w]);
+      }
+      const float v = *(lds_float_t)(from + Ring::kLse + u * 256 + c * 4);
+      // no row, or one that sees nothing: its powers are 0
+      const bool none = row >= rows || v == -__builtin_inff();
+      const float ls = v * 1.4426950408889634f;
+      const int p = pos0 + token_of(min(row, rows - 1));
+      const bool all = !__ballot(none || (a.causal && p < j0 + 63));
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < C::KW; ++w)
 #pragma unroll
-          for (int u = 0; u < C::kTerms; ++u) sc = mfma16(kk[h][w], q[w][u], sc);
+          for (int t = 0; t < C::kTerms; ++t) sc = mfma16(kk[h][w], q[w][t], sc);
         if (!all) {
           const int last = none ? -1 : a.causal ? p - (j0 + 16 * h + 4 * g) : 4;
 #pragma unroll
@@ -1371,20 +1407,6 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_many_kernel(Attn4Args
 #pragma unroll
           for (int r = 0; r < 4; ++r) acc[h][r] += __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale2, -ls));
         }
-      }
-    };
-    int r0 = first + wr * 16;
-    if (r0 < rows) {
-      load(r0, qa, la, ta);
-      while (true) {
-        load(r0 + 16 * C::WR, qb, lb, tb);
-        use(qa, la, ta);
-        r0 += 16 * C::WR;
-        if (r0 >= rows) break;
-        load(r0 + 16 * C::WR, qa, la, ta);
-        use(qb, lb, tb);
-        r0 += 16 * C::WR;
-        if (r0 >= rows) break;
       }
     }
   }
@@ -1398,14 +1420,15 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_many_kernel(Attn4Args
       got = c == 4 * h + r ? v : got;
     }
   if constexpr (C::WR > 1) {
-    s_sum[wave][lane] = got;
+    __syncthreads();  // the last rows have been read
+    *(lds_float_t)(attn4_smem + wave * 256 + lane * 4) = got;
     __syncthreads();
     if (wr != 0) return;
     got = 0.f;
 #pragma unroll
-    for (int w = 0; w < C::WR; ++w) got += s_sum[wk * C::WR + w][lane];
+    for (int w = 0; w < C::WR; ++w) got += *(lds_float_t)(attn4_smem + (wk * C::WR + w) * 256 + lane * 4);
   }
-  if (any && j < hi && my_page >= 0 && my_page < a.pages) {
+  if (my_page >= 0 && my_page < a.pages) {
     float* w = a.weights + weight_at(a, my_page, head, j);
     *w = (j < pos0 ? a.decay * *w : 0.f) + got;
   }
