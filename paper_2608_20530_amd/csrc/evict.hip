@@ -20,7 +20,7 @@ namespace {
 constexpr int kEvictMaxN = 4096;
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
 constexpr int kKeys = 32;  // weights that a thread keeps
-constexpr int kBins = 2048;
+constexpr int kBins = 2048, kCopies = 4;
 constexpr int kMoveThreads = 512;
 
 struct EvictArgs {
@@ -69,7 +69,8 @@ __device__ __forceinline__ int group_sum(int v, int* s) {
 }
 
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-  __shared__ int s_bins[kBins];
+  __shared__ int s_copy[kCopies][kBins];  // histograms: a wave adds to one of them
+  int* const s_bins = s_copy[0];
   __shared__ int s_wave[2][kSelectWaves];
   __shared__ int s_count[2][kKeys][kSelectWaves];
   __shared__ int s_found[2];
@@ -140,8 +141,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = kShift[pass];
     const uint32_t mask = (1u << kBits[pass]) - 1;
-    for (int i = tid; i < kBins; i += kSelectThreads) s_bins[i] = 0;
+    for (int i = tid; i < kCopies * kBins; i += kSelectThreads) s_bins[i] = 0;
     __syncthreads();
+    int* const mine = s_copy[wave % kCopies];
     for (int s = 0; s < stretches; ++s) {
       const int j0 = s * kStretch;
       if (stretches > 1) read(j0);
@@ -156,15 +158,20 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
         if (!on) continue;
         const uint32_t b0 = readlane32(bin, __builtin_ctzll(on));
         if (__ballot(in && bin == b0) == on) {
-          if (lane == 0) atomicAdd(&s_bins[b0], (int)__popcll(on));
+          if (lane == 0) atomicAdd(&mine[b0], (int)__popcll(on));
         } else if (in) {
-          atomicAdd(&s_bins[bin], 1);
+          atomicAdd(&mine[bin], 1);
         }
       }
     }
     __syncthreads();
     // the bin, from the top, in which the need-th key lies: each thread has the bins 2 x and 2 x + 1 from the top
-    const int hi = s_bins[kBins - 1 - 2 * tid], lo = s_bins[kBins - 2 - 2 * tid];
+    int hi = 0, lo = 0;
+#pragma unroll
+    for (int y = 0; y < kCopies; ++y) {
+      hi += s_copy[y][kBins - 1 - 2 * tid];
+      lo += s_copy[y][kBins - 2 - 2 * tid];
+    }
     int sum = hi + lo;
 #pragma unroll
     for (int m = 1; m < kWave; m <<= 1) {

@@ -393,11 +393,30 @@ __device__ __forceinline__ Code4 quantise(const u32x4_t& w) {
 }
 
 // A key in 64 bits, from its elements on: sums, norm, rotation, scale and codes. No contraction: each operation is
-// rounded as it stands in the formula.
+// rounded as it stands in the formula. `weight` and `weight_p` at the lane's and its partner's elements, or NULL; `angles`
+// at its pairs' cosines.
 template <typename T, int LPH>
-__device__ __forceinline__ Code4 quantise64(const u32x4_t& w, bool norm, const float (&wt)[8], const float (&wp)[8],
-                                            const RopeLane& r, int d, float eps, int rot, int interleaved) {
+__device__ __forceinline__ Code4 quantise64(const u32x4_t& w, const float* weight, const float* weight_p, const float* angles,
+                                            int partner, bool turned, bool upper, int d, float eps, int rot,
+                                            int interleaved) {
 #pragma clang fp contract(off)
+  const bool norm = weight != nullptr;
+  float wt[8], wp[8];
+  RopeLane r;
+  r.partner = partner;
+  r.turned = turned;
+  r.upper = upper;
+  if (norm) {
+    load_floats<8>(weight, wt);
+    load_floats<8>(weight_p, wp);
+  }
+  if (rot && interleaved) {
+    load_floats<4>(angles, r.cs);
+    load_floats<4>(angles + rot / 2, r.sn);
+  } else if (rot) {
+    load_floats<8>(angles, r.cs);
+    load_floats<8>(angles + rot / 2, r.sn);
+  }
   double x[8], s = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -465,17 +484,18 @@ __device__ __forceinline__ Code4 quantise64(const u32x4_t& w, bool norm, const f
   return {out, (uint32_t)b};
 }
 
-// A key: in fp32, and again in 64 bits by the whole wave where some element's scale, code or sign is not certain. An
+// A key in fp32, and whether some element's scale, code or sign is not certain: then it is done again in 64 bits. An
 // element is at most 2^-20 of the magnitudes that it was made from off (sum of squares 13 roundings, halved by the
 // root; mean, root, two factors, two products and a sum: 16 in all of 2^-24), so it is certain where four times that
-// up or down changes nothing. With normal values one wave in 400 is done again.
+// up or down changes nothing. With normal values one step of a wave in 400 is done again.
 constexpr float kUncertain = 0x1p-18f;
 template <typename T, int LPH>
 __device__ __forceinline__ Code4 quantise_key(const u32x4_t& w, bool norm, const float (&wt)[8], const float (&wp)[8],
-                                              const RopeLane& r, int d, float eps, int rot, int interleaved) {
+                                              const RopeLane& r, int d, float eps, int rot, int interleaved,
+                                              bool& unsure) {
   float y[8], size[8], lo[8], hi[8], most_lo = 0.f, most_hi = 0.f;
   norm_turn32<T, LPH, true>(w, norm, wt, wp, r, d, eps, rot, interleaved, y, size);
-  bool unsure = false;
+  unsure = false;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float off = size[i] * kUncertain, v = fabsf(y[i]);
@@ -490,14 +510,12 @@ __device__ __forceinline__ Code4 quantise_key(const u32x4_t& w, bool norm, const
   const uint32_t s = scale4(most_lo);
   unsure |= !(most_hi < 0x1p126f) || s != scale4(most_hi);
   const float scale = scale_of(s);
-  const uint32_t low = codes4(lo, scale);
-  unsure |= low != codes4(hi, scale);
-  if (__ballot(unsure)) return quantise64<T, LPH>(w, norm, wt, wp, r, d, eps, rot, interleaved);
+  unsure |= codes4(lo, scale) != codes4(hi, scale);
   return {codes4(y, scale), s};
 }
 
 template <typename T, int LPH, bool FOUR>
-__global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) {
+__global__ __launch_bounds__(kRopeThreads, FOUR ? 4 : 1) void qk_norm_rope_kernel(RopeArgs a) {
   constexpr int kHeads = kWave / LPH;  // heads a wave holds
   const int lane = lane_id(), l = lane % LPH, g = lane / LPH;
   const int e0 = l * 8;
@@ -527,7 +545,13 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
   const int wave = (int)uniform32(threadIdx.x / kWave);
   const int waves = (int)gridDim.x * (kRopeThreads / kWave);
   const int64_t items = a.tokens * a.parts;
-  for (int64_t it = (int64_t)blockIdx.x * (kRopeThreads / kWave) + wave; it < items; it += waves) {
+  // 4 bits: the wave's steps whose keys have to be done again in 64 bits, as (round, step); with more than kAgain of them
+  // all keys are. They are done after the rest, so that they cost the rest no registers (within it: 229 of them, and
+  // 119 us for 16381 tokens).
+  constexpr int kAgain = 64;
+  __shared__ uint32_t s_again[FOUR ? kRopeThreads / kWave : 1][FOUR ? kAgain : 1];
+  uint32_t again = 0, round = 0;
+  for (int64_t it = (int64_t)blockIdx.x * (kRopeThreads / kWave) + wave; it < items; it += waves, ++round) {
     const int64_t t = it / a.parts;
     const int part = (int)(it - t * a.parts);
     const int s0 = steps * part / a.parts, s1 = steps * (part + 1) / a.parts;
@@ -583,8 +607,13 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
           const bool is_k = s + u < qs + ks;
           const int h = (is_k ? s + u - qs : s + u - qs - ks) * kHeads + g;
           if constexpr (FOUR) {
-            const Code4 y = is_k ? quantise_key<T, LPH>(x[u], norm_k, kw, kp, r, a.d, a.eps, a.rot, a.interleaved)
+            bool unsure = false;
+            const Code4 y = is_k ? quantise_key<T, LPH>(x[u], norm_k, kw, kp, r, a.d, a.eps, a.rot, a.interleaved, unsure)
                                  : quantise<T>(x[u]);
+            if (__ballot(unsure)) {
+              if (again < kAgain) s_again[wave][again] = round * steps + (s + u);
+              ++again;
+            }
             const int64_t to = at + (int64_t)h * a.head_stride;
             if (mine && h < a.kv_heads) {
               *reinterpret_cast<uint32_t*>((unsigned char*)(is_k ? a.k_cache : a.v_cache) + to + l * 4) = y.w;
@@ -597,6 +626,33 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
           uint16_t* dst = (is_k ? a.k_cache : a.v_cache) + at + (int64_t)h * a.head_stride;
           if (mine && h < a.kv_heads) *reinterpret_cast<u32x4_t*>(dst + e0) = y;
         }
+      }
+    }
+  }
+  if constexpr (FOUR) {
+    const int64_t first = (int64_t)blockIdx.x * (kRopeThreads / kWave) + wave;
+    const uint32_t all = round * (uint32_t)steps;  // (round, step) of all of the wave's rounds
+    const bool listed = again <= kAgain;
+    for (uint32_t i = 0; i < (listed ? again : all); ++i) {
+      const uint32_t which = uniform32(listed ? s_again[wave][i] : i);
+      const int64_t it = first + (int64_t)(which / steps) * waves, t = it / a.parts;
+      const int s = (int)(which % steps), part = (int)(it - t * a.parts);
+      if (s < qs || s >= qs + ks || s < steps * part / a.parts || s >= steps * (part + 1) / a.parts) continue;
+      const int pos = a.positions[t], slot = a.slots[t];
+      const int page = slot < 0 ? -1 : slot / a.page_size;
+      if (pos < 0 || (a.rot && pos >= a.max_positions) || page < 0 || page >= a.pages) continue;
+      const int h = (s - qs) * kHeads + g;
+      u32x4_t x = {0, 0, 0, 0};
+      if (mine && h < a.kv_heads) x = *reinterpret_cast<const u32x4_t*>(a.k + t * a.k_stride + (int64_t)h * a.d + e0);
+      const int p0 = !r.turned ? 0 : a.interleaved ? e0 / 2 : r.upper ? e0 - half : e0;
+      const Code4 y = quantise64<T, LPH>(x, norm_k ? a.k_weight + (mine ? e0 : 0) : nullptr,
+                                         norm_k ? a.k_weight + (mine ? po : 0) : nullptr,
+                                         a.rot ? a.cos_sin + (int64_t)pos * a.rot + p0 : nullptr, r.partner, r.turned,
+                                         r.upper, a.d, a.eps, a.rot, a.interleaved);
+      const int64_t to = page * a.page_stride + (int64_t)(slot - page * a.page_size) * a.token_stride + (int64_t)h * a.head_stride;
+      if (mine && h < a.kv_heads) {
+        *reinterpret_cast<uint32_t*>((unsigned char*)a.k_cache + to + l * 4) = y.w;
+        if (l % 4 == 0) a.k_scales[to / 16 + l / 4] = (unsigned char)y.scale;
       }
     }
   }
