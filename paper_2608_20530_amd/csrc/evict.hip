@@ -20,7 +20,7 @@ namespace {
 constexpr int kEvictMaxN = 4096;
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
 constexpr int kKeys = 32;  // weights that a thread keeps
-constexpr int kBins = 2048, kCopies = 4;
+constexpr int kBins = 2048;
 constexpr int kMoveThreads = 512;
 
 struct EvictArgs {
@@ -36,7 +36,7 @@ struct EvictArgs {
   int N, M, P, C, heads, d, n_pages;
   uint32_t page_mul, page_shift;
   int budget, limit, sinks, recent, max_length;
-  int parts;  // workgroups that share a request and head's columns
+  int parts;  // workgroups that share a request and head's columns: 1, or one for each
 };
 
 struct EvictRow {
@@ -69,8 +69,7 @@ __device__ __forceinline__ int group_sum(int v, int* s) {
 }
 
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-  __shared__ int s_copy[kCopies][kBins];  // histograms: a wave adds to one of them
-  int* const s_bins = s_copy[0];
+  __shared__ int s_bins[kBins];
   __shared__ int s_wave[2][kSelectWaves];
   __shared__ int s_count[2][kKeys][kSelectWaves];
   __shared__ int s_found[2];
@@ -112,25 +111,34 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   const int32_t* trow = a.table + (int64_t)n * a.M;
   const int first = a.sinks, last = row.length - a.recent;  // the tokens that weights decide about
   int need = a.budget - a.sinks - a.recent;
-  auto slot_of = [&](int j) {
-    const int e = evict_entry(a, j), page = trow[e];
-    return page >= 0 && page < a.n_pages ? page * a.P + (j - e * a.P) : -1;
-  };
-  // the weight's order, greater for the heavier; a token without a page comes last
-  auto key_of = [&](int j) -> uint32_t {
-    const int e = evict_entry(a, j), page = trow[e];
-    if (page < 0 || page >= a.n_pages) return 0;
-    return order_bits(a.weights[((int64_t)page * a.heads + head) * a.P + (j - e * a.P)]);
-  };
   // Tokens in stretches of kSelectThreads * kKeys. One stretch is the rule, and its keys are read once.
   constexpr int kStretch = kSelectThreads * kKeys;
   const int stretches = (row.length + kStretch - 1) / kStretch;
+  // The weights' order, greater for the heavier (a token without a page comes last), and slots. Eight loads at a time
+  // under way, pages and then weights: one by one they are 64 round trips (62 us for 32768 tokens).
   uint32_t key[kKeys];
+  int slot[kKeys];
   auto read = [&](int j0) {
+    constexpr int kAtOnce = 8;
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-      const int j = j0 + i * kSelectThreads + tid;
-      if (j0 + i * kSelectThreads < row.length) key[i] = j >= first && j < last ? key_of(j) : 0;
+    for (int i0 = 0; i0 < kKeys; i0 += kAtOnce) {
+      if (j0 + i0 * kSelectThreads >= row.length) break;
+      int page[kAtOnce], o[kAtOnce];
+      float w[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int j = min(j0 + (i0 + i) * kSelectThreads + tid, row.length - 1), e = evict_entry(a, j);
+        page[i] = trow[e];
+        o[i] = j - e * a.P;
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const bool there = page[i] >= 0 && page[i] < a.n_pages;
+        slot[i0 + i] = there ? page[i] * a.P + o[i] : -1;
+        w[i] = a.weights[((int64_t)(there ? page[i] : 0) * a.heads + head) * a.P + o[i]];
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) key[i0 + i] = slot[i0 + i] < 0 ? 0 : order_bits(w[i]);
     }
   };
   if (stretches == 1) read(0);
@@ -141,9 +149,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = kShift[pass];
     const uint32_t mask = (1u << kBits[pass]) - 1;
-    for (int i = tid; i < kCopies * kBins; i += kSelectThreads) s_bins[i] = 0;
+    for (int i = tid; i < kBins; i += kSelectThreads) s_bins[i] = 0;
     __syncthreads();
-    int* const mine = s_copy[wave % kCopies];
     for (int s = 0; s < stretches; ++s) {
       const int j0 = s * kStretch;
       if (stretches > 1) read(j0);
@@ -158,20 +165,15 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
         if (!on) continue;
         const uint32_t b0 = readlane32(bin, __builtin_ctzll(on));
         if (__ballot(in && bin == b0) == on) {
-          if (lane == 0) atomicAdd(&mine[b0], (int)__popcll(on));
+          if (lane == 0) atomicAdd(&s_bins[b0], (int)__popcll(on));
         } else if (in) {
-          atomicAdd(&mine[bin], 1);
+          atomicAdd(&s_bins[bin], 1);
         }
       }
     }
     __syncthreads();
     // the bin, from the top, in which the need-th key lies: each thread has the bins 2 x and 2 x + 1 from the top
-    int hi = 0, lo = 0;
-#pragma unroll
-    for (int y = 0; y < kCopies; ++y) {
-      hi += s_copy[y][kBins - 1 - 2 * tid];
-      lo += s_copy[y][kBins - 2 - 2 * tid];
-    }
+    const int hi = s_bins[kBins - 1 - 2 * tid], lo = s_bins[kBins - 2 - 2 * tid];
     int sum = hi + lo;
 #pragma unroll
     for (int m = 1; m < kWave; m <<= 1) {
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
       const uint64_t below = (1ull << lane) - 1;
       const int m0 = base_more + s_count[0][i][wave] + (int)__popcll(__ballot(more) & below);
       const int e0 = base_equal + s_count[1][i][wave] + (int)__popcll(__ballot(equal) & below);
-      if (more || (equal && e0 < need)) list[m0 + min(e0, need)] = slot_of(j0 + i * kSelectThreads + tid);
+      if (more || (equal && e0 < need)) list[m0 + min(e0, need)] = slot[i];
     }
     base_more += s_found[0];
     base_equal += s_found[1];
@@ -255,17 +257,19 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   }
 }
 
-// A row of a head is columns of 16 bytes: d / 32 of the key, d / 32 of the value; then one column each for the keys'
-// scales, the values' scales and the weight. A thread holds kHold columns of a stretch.
-constexpr int kHold = 8;
+// A row of a head is columns of 16 bytes, d / 32 of the key and d / 32 of the value, and three narrow ones: the keys' scales,
+// the values' scales and the weight. One workgroup moves all of a request and head, or each column has its own. A thread
+// holds kHold columns of a stretch and kNarrow narrow ones. All loads of a kind are under way together.
+constexpr int kHold = 8, kNarrow = 4;
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
   const int tid = threadIdx.x;
   const int part = (int)blockIdx.x % a.parts, nh = (int)blockIdx.x / a.parts;
   const int n = nh / a.heads, head = nh % a.heads;
   if (!evict_row(a, n).cut) return;
   const int wide = a.d / kBlock4;  // 16-byte columns of a key; also scale bytes
-  const int columns = 2 * wide + 3;
-  const int c0 = columns * part / a.parts, cs = columns * (part + 1) / a.parts - c0;
+  const bool alone = a.parts == 1;
+  const int c0 = alone ? 0 : part, cs = alone ? 2 * wide : part < 2 * wide ? 1 : 0;  // wide columns, and narrow ones
+  const int k0 = alone ? 0 : part - 2 * wide, kinds = alone ? 3 : part < 2 * wide ? 0 : 1;
   const int32_t* list = a.list + (int64_t)nh * a.budget;
   const int32_t* trow = a.table + (int64_t)n * a.M;
   const int64_t ho = (int64_t)head * a.head_stride;
@@ -277,52 +281,78 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
     const int page = evict_entry(a, slot);
     return a.weights + ((int64_t)page * a.heads + head) * a.P + (slot - page * a.P);
   };
-  auto scales = [&](unsigned char* at) {  // d / 32 bytes
-    uint64_t w = 0;
-    for (int b = 0; b < wide; ++b) w |= (uint64_t)at[b] << (8 * b);
-    return w;
-  };
   // tokens of a stretch
-  const int rows = kMoveThreads * kHold / cs;
+  const int rows = min(cs ? kMoveThreads * kHold / cs : 1 << 30, kinds ? kMoveThreads * kNarrow / kinds : 1 << 30);
   for (int i0 = 0; i0 < a.budget; i0 += rows) {
-    const int here = min(rows, a.budget - i0), items = here * cs;
-    u32x4_t held[kHold];
-    int64_t to[kHold];  // slot of the place, -1 for nothing to do
+    const int here = min(rows, a.budget - i0), items = here * cs, narrows = here * kinds;
+    int from[kHold], to[kHold], nfrom[kNarrow], nto[kNarrow];  // slots; `to` is -1 where there is nothing to do
+    auto places = [&](int item, int count, int per, int& src, int& dst) {
+      const int i = i0 + min(item, count - 1) / per, e = evict_entry(a, i);
+      src = list[i];
+      dst = trow[e];  // its page
+    };
+    auto settle = [&](int item, int count, int per, int& src, int& dst) {
+      const int i = i0 + min(item, count - 1) / per, e = evict_entry(a, i);
+      const int slot = dst >= 0 && dst < a.n_pages ? dst * a.P + (i - e * a.P) : -1;
+      dst = item >= count || src < 0 || src == slot ? -1 : slot;
+      src = max(src, 0);
+    };
+    if (cs) {
 #pragma unroll
-    for (int x = 0; x < kHold; ++x) {
-      const int item = x * kMoveThreads + tid;
-      to[x] = -1;
-      if (item >= items) continue;
-      const int r = item / cs, c = c0 + item - r * cs, i = i0 + r;
-      const int from = list[i], e = evict_entry(a, i), page = trow[e];
-      const int slot = page >= 0 && page < a.n_pages ? page * a.P + (i - e * a.P) : -1;
-      if (from < 0 || slot < 0 || from == slot) continue;
-      to[x] = slot;
-      if (c < 2 * wide) {
-        held[x] = *reinterpret_cast<const u32x4_t*>((c < wide ? a.k : a.v) + offset(from) + (c % wide) * 16);
-      } else if (c < 2 * wide + 2) {
-        const uint64_t w = scales((c == 2 * wide ? a.ks : a.vs) + offset(from) / 16);
-        held[x][0] = (uint32_t)w;
-        held[x][1] = (uint32_t)(w >> 32);
-      } else {
-        held[x][0] = __float_as_uint(*weight(from));
+      for (int x = 0; x < kHold; ++x) places(x * kMoveThreads + tid, items, cs, from[x], to[x]);
+    }
+    if (kinds) {
+#pragma unroll
+      for (int x = 0; x < kNarrow; ++x) places(x * kMoveThreads + tid, narrows, kinds, nfrom[x], nto[x]);
+    }
+    u32x4_t held[kHold];
+    if (cs) {
+#pragma unroll
+      for (int x = 0; x < kHold; ++x) {
+        settle(x * kMoveThreads + tid, items, cs, from[x], to[x]);
+        const int c = c0 + (x * kMoveThreads + tid) % cs;
+        held[x] = *reinterpret_cast<const u32x4_t*>((c < wide ? a.k : a.v) + offset(from[x]) + (c % wide) * 16);
+      }
+    }
+    uint32_t small[kNarrow][8];
+    if (kinds) {
+#pragma unroll
+      for (int x = 0; x < kNarrow; ++x) {
+        const int kind = k0 + (x * kMoveThreads + tid) % kinds;
+        settle(x * kMoveThreads + tid, narrows, kinds, nfrom[x], nto[x]);
+        if (kind < 2) {
+          const unsigned char* at = (kind == 0 ? a.ks : a.vs) + offset(nfrom[x]) / 16;
+#pragma unroll
+          for (int b = 0; b < 8; ++b) small[x][b] = at[min(b, wide - 1)];
+        } else {
+          small[x][0] = __float_as_uint(*weight(nfrom[x]));
+        }
       }
     }
     // everything that this stretch overwrites has been read, by every wave
     __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
+    if (cs) {
 #pragma unroll
-    for (int x = 0; x < kHold; ++x) {
-      if (to[x] < 0) continue;
-      const int item = x * kMoveThreads + tid, c = c0 + item % cs, slot = (int)to[x];
-      if (c < 2 * wide) {
-        *reinterpret_cast<u32x4_t*>((c < wide ? a.k : a.v) + offset(slot) + (c % wide) * 16) = held[x];
-      } else if (c < 2 * wide + 2) {
-        unsigned char* at = (c == 2 * wide ? a.ks : a.vs) + offset(slot) / 16;
-        const uint64_t w = (uint64_t)held[x][1] << 32 | held[x][0];
-        for (int b = 0; b < wide; ++b) at[b] = (unsigned char)(w >> (8 * b));
-      } else {
-        *weight(slot) = __uint_as_float(held[x][0]);
+      for (int x = 0; x < kHold; ++x) {
+        if (to[x] < 0) continue;
+        const int c = c0 + (x * kMoveThreads + tid) % cs;
+        *reinterpret_cast<u32x4_t*>((c < wide ? a.k : a.v) + offset(to[x]) + (c % wide) * 16) = held[x];
+      }
+    }
+    if (kinds) {
+#pragma unroll
+      for (int x = 0; x < kNarrow; ++x) {
+        if (nto[x] < 0) continue;
+        const int kind = k0 + (x * kMoveThreads + tid) % kinds;
+        if (kind < 2) {
+          unsigned char* at = (kind == 0 ? a.ks : a.vs) + offset(nto[x]) / 16;
+#pragma unroll
+          for (int b = 0; b < 8; ++b)
+            if (b < wide) at[b] = (unsigned char)small[x][b];
+        } else {
+          *weight(nto[x]) = __uint_as_float(small[x][0]);
+        }
       }
     }
   }
@@ -405,8 +435,8 @@ extern "C" lilicorr_status lilicorr_evict(const lilicorr_evict_args* args, hipSt
   const int64_t groups = x.N * c.heads;
   hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)groups), dim3(kSelectThreads), 0, stream, a);
   if (a.max_length > x.limit) {
-    const int64_t columns = 2 * (c.d / kBlock4) + 3, want = 512 / groups;
-    a.parts = (int)(want < 1 ? 1 : want < columns ? want : columns);
+    // few requests and heads: a workgroup for each column (one conversation with 8 heads 24 us, 57 with four columns each)
+    a.parts = groups >= 256 ? 1 : 2 * (c.d / kBlock4) + 3;
     hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(groups * a.parts)), dim3(kMoveThreads), 0, stream, a);
   }
   return launch_status();
