@@ -633,9 +633,10 @@ lilicorr_status lilicorr_prefix_attention(const lilicorr_attention_args *args, h
  *
  * An element is E2M1 (a sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6), two to a byte, the even element in the low half. 32
  * neighbouring elements of a head are a block with a scale byte b, 1 to 252: they stand for their values times
- * 2^(b - 127). A block whose b is 255 is NaN throughout; 0, 253 and 254 are never written. Element x of head h of the token at place o of page p lies at byte
- * p * page_stride + o * token_stride + h * head_stride + x / 2 of k (keys) and of v (values), its scale at a sixteenth
- * of that offset (without x / 2) + x / 32 of k_scales and v_scales: scales are laid out as codes are.
+ * 2^(b - 127). A block whose b is 255 is NaN throughout; 0, 253 and 254 are never written. Element x of head h of the
+ * token at place o of page p lies at byte p * page_stride + o * token_stride + h * head_stride + x / 2 of k (keys) and of
+ * v (values), its scale at a sixteenth of that offset (without x / 2) + x / 32 of k_scales and v_scales: scales are laid
+ * out as codes are.
  */
 typedef struct {
     void *k, *v;              /* codes, 16-byte aligned */
@@ -644,7 +645,7 @@ typedef struct {
     int heads;                /* key heads */
     int d;                    /* head width: a multiple of 32, at most 256 */
     int64_t pages;
-    int64_t page_stride, token_stride, head_stride; /* bytes of codes, multiples of 16 */
+    int64_t page_stride, token_stride, head_stride; /* bytes of codes, multiples of 16; token_stride below 2^27 */
 } lilicorr_cache4;
 
 /*
@@ -653,7 +654,7 @@ typedef struct {
  * power of two s with max |x| <= 7 s, within 2^-126 .. 2^125, and each element the code nearest to x / s, ties to the
  * even code, what is over 6 s to 6 s (so that no element is more than s off, short of the range's ends). Keys and
  * their scales are those of the arithmetic in 64 bits. A block that holds an infinity or a NaN becomes NaN.
- * Limits as for lilicorr_qk_norm_rope; the cache must not overlap q, k or v.
+ * Limits as for lilicorr_qk_norm_rope; the cache must not overlap q, k, v or q_out.
  */
 typedef struct {
     const void *q, *k, *v;
@@ -677,7 +678,8 @@ lilicorr_status lilicorr_qk_norm_rope4(const lilicorr_qk_norm_rope4_args *args, 
  * NaN blocks among them; a NaN block of values that it sees makes those 32 elements of its output NaN.
  *   lse   [tokens][heads] fp32 or NULL: the natural logarithm of each row's sum of exponentials, log sum_j exp(scale
  *         q . k_j), of the probabilities before they are rounded; -inf where it sees no key. For
- *         lilicorr_key_weights. 4-byte aligned. Neither out nor lse may overlap q's rows or one another.
+ *         lilicorr_key_weights. 4-byte aligned.
+ * out, lse and the workspace must not overlap what the call reads, nor one another.
  */
 typedef struct {
     const void *q;                  /* [tokens][heads][d] */

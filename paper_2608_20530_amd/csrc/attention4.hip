@@ -325,11 +325,18 @@ extern "C" lilicorr_status lilicorr_window_attention4(const lilicorr_attention4_
     return LILICORR_ERR_ALIGNMENT;
   if (!x.workspace || x.workspace_bytes < p.bytes) return LILICORR_ERR_WORKSPACE;
   if (x.max_tokens == 0) return LILICORR_OK;
-  const size_t row = (size_t)x.heads * c.d * 2, out = row * (size_t)x.tokens;
-  const size_t lse = x.lse ? (size_t)x.heads * (size_t)x.tokens * 4 : 0;
-  if (rows_overlap(x.q, x.q_stride * 2, row, x.tokens, x.out, out) || overlap(x.out, out, x.lse, lse) ||
-      (lse && rows_overlap(x.q, x.q_stride * 2, row, x.tokens, x.lse, lse)))
-    return LILICORR_ERR_INVALID_ARG;
+  // what is written must not lie on what other waves still read or write
+  const size_t row = (size_t)x.heads * c.d * 2, span = cache4_span(c);
+  const struct { const void* at; size_t bytes; } parts[] = {
+      {x.out, row * (size_t)x.tokens}, {x.lse, x.lse ? (size_t)x.heads * (size_t)x.tokens * 4 : 0}, {x.workspace, p.bytes},
+      {c.k, span}, {c.v, span}, {c.k_scales, cache4_scales(span)}, {c.v_scales, cache4_scales(span)},
+      {x.table, (size_t)x.N * x.table_width * 4}, {x.starts, ((size_t)x.N + 1) * 4}, {x.totals, (size_t)x.N * 4}};
+  constexpr int kWritten = 3, kParts = sizeof(parts) / sizeof(parts[0]);
+  for (int i = 0; i < kWritten; ++i) {
+    if (rows_overlap(x.q, x.q_stride * 2, row, x.tokens, parts[i].at, parts[i].bytes)) return LILICORR_ERR_INVALID_ARG;
+    for (int j = i + 1; j < kParts; ++j)
+      if (overlap(parts[i].at, parts[i].bytes, parts[j].at, parts[j].bytes)) return LILICORR_ERR_INVALID_ARG;
+  }
   return x.dtype == LILICORR_BF16 ? run4<Bf16>(x, p, stream) : run4<F16>(x, p, stream);
 }
 

@@ -545,13 +545,13 @@ __global__ __launch_bounds__(kRopeThreads, FOUR ? 4 : 1) void qk_norm_rope_kerne
   const int wave = (int)uniform32(threadIdx.x / kWave);
   const int waves = (int)gridDim.x * (kRopeThreads / kWave);
   const int64_t items = a.tokens * a.parts;
-  // 4 bits: the wave's steps whose keys have to be done again in 64 bits, as (round, step); with more than kAgain of them
+  // 4 bits: the wave's steps whose keys have to be done again in 64 bits, as (turn, step); with more than kAgain of them
   // all keys are. They are done after the rest, so that they cost the rest no registers (within it: 229 of them, and
   // 119 us for 16381 tokens).
   constexpr int kAgain = 64;
   __shared__ uint32_t s_again[FOUR ? kRopeThreads / kWave : 1][FOUR ? kAgain : 1];
-  uint32_t again = 0, round = 0;
-  for (int64_t it = (int64_t)blockIdx.x * (kRopeThreads / kWave) + wave; it < items; it += waves, ++round) {
+  uint32_t again = 0, turn = 0;
+  for (int64_t it = (int64_t)blockIdx.x * (kRopeThreads / kWave) + wave; it < items; it += waves, ++turn) {
     const int64_t t = it / a.parts;
     const int part = (int)(it - t * a.parts);
     const int s0 = steps * part / a.parts, s1 = steps * (part + 1) / a.parts;
@@ -611,7 +611,7 @@ __global__ __launch_bounds__(kRopeThreads, FOUR ? 4 : 1) void qk_norm_rope_kerne
             const Code4 y = is_k ? quantise_key<T, LPH>(x[u], norm_k, kw, kp, r, a.d, a.eps, a.rot, a.interleaved, unsure)
                                  : quantise<T>(x[u]);
             if (__ballot(unsure)) {
-              if (again < kAgain) s_again[wave][again] = round * steps + (s + u);
+              if (again < kAgain) s_again[wave][again] = turn * steps + (s + u);
               ++again;
             }
             const int64_t to = at + (int64_t)h * a.head_stride;
@@ -631,7 +631,7 @@ __global__ __launch_bounds__(kRopeThreads, FOUR ? 4 : 1) void qk_norm_rope_kerne
   }
   if constexpr (FOUR) {
     const int64_t first = (int64_t)blockIdx.x * (kRopeThreads / kWave) + wave;
-    const uint32_t all = round * (uint32_t)steps;  // (round, step) of all of the wave's rounds
+    const uint32_t all = turn * (uint32_t)steps;  // (turn, step) of all of the wave's turns
     const bool listed = again <= kAgain;
     for (uint32_t i = 0; i < (listed ? again : all); ++i) {
       const uint32_t which = uniform32(listed ? s_again[wave][i] : i);

@@ -550,3 +550,208 @@ def test_evict_twice_and_with_given_outputs(lib):
     x.update(totals=e.totals, pages=e.pages, cursor=e.cursor)
     again = check_evict(lib, x, 100, 200, 4, 16)
     assert again.totals.tolist() == [100, 50] and again.evicted.tolist() == [0, 0]
+
+
+# ---- long contexts of many requests: a workgroup's waves share a token's key heads -----------------------------
+
+def widened(x, N, keys):
+    """The same requests among N, the others without tokens, in a table with room for `keys` tokens of each."""
+    page = x["cache"].k.shape[1]
+    n, m = x["table"].shape
+    table = torch.full((N, -(-keys // page)), -1, dtype=torch.int32, device="cuda")
+    table[:n, :m] = x["table"]
+    last = x["starts"][-1:]
+    return dict(x, table=table, starts=torch.cat((x["starts"], last.expand(N - n))).contiguous(),
+                totals=torch.cat((x["totals"], torch.zeros(N - n, dtype=torch.int32, device="cuda"))))
+
+
+LONG_CASES = [
+    # new, ctx, Hq, Hkv, d, page, window, sinks, causal, dtype, N, keys
+    ([1, 1, 1, 1], [0, 31, 700, 2000], 16, 4, 64, 16, 0, 0, True, BF, 64, 8192),
+    ([1, 1, 1], [33, 1500, 800], 32, 8, 128, 16, 0, 0, True, HF, 64, 8192),
+    ([2, 1], [1000, 63], 8, 4, 256, 32, 0, 0, True, BF, 64, 8192),
+    ([4, 3], [900, 40], 32, 4, 128, 48, 0, 0, False, BF, 64, 8208),
+    ([4, 2, 0, 1], [500, 1200, 9, 0], 32, 4, 64, 16, 0, 0, True, HF, 64, 8192),
+    ([16, 9], [700, 90], 16, 4, 128, 16, 0, 0, True, BF, 64, 8192),
+    ([16, 5], [300, 1100], 8, 2, 64, 16, 0, 0, False, HF, 128, 8192),
+    ([8, 2], [400, 900], 8, 2, 256, 16, 0, 0, True, BF, 128, 8192),
+    ([1, 1, 1], [300, 90, 33], 16, 4, 128, 16, 64, 4, True, BF, 8192, 400),
+    ([4, 4], [300, 70], 32, 4, 64, 16, 40, 3, True, HF, 8192, 400),
+    ([16, 16], [200, 333], 16, 4, 128, 32, 90, 20, True, BF, 8192, 400),
+    ([2], [200], 32, 4, 256, 16, 33, 0, True, HF, 8192, 400),
+]
+
+
+@pytest.mark.parametrize("new,ctx,Hq,Hkv,d,page,window,sinks,causal,dtype,N,keys", LONG_CASES)
+def test_many_keys_in_all(lib, new, ctx, Hq, Hkv, d, page, window, sinks, causal, dtype, N, keys):
+    print("many keys", new[:4], ctx[:4], Hq, Hkv, d, page, window, sinks, flush=True)
+    x = attention_inputs(lib, new, ctx, Hq, Hkv, d, page, dtype)
+    mask = dict(window=window, sinks=sinks, causal=causal)
+    y = widened(x, N, keys)
+    got = attend(lib, y, **mask, max_tokens=max(new), max_length=keys)
+    check_attention(x, got, wanted(x, **mask))
+    if window:
+        return
+    before = torch.rand(x["cache"].k.shape[0], Hkv, page, generator=torch.Generator().manual_seed(2)).cuda()
+    weights = lib.key_weights(y["q"], got[1], y["cache"], y["table"], y["starts"], y["totals"], before.clone(),
+                              causal=causal, decay=0.75, max_tokens=max(new), max_length=keys)
+    torch.cuda.synchronize()
+    want = ref.key_weights(f64(x["q"]), f64(got[1]), values(x["cache"])[0],
+                           *(host(x[k]) for k in ("table", "starts", "totals")), host(before), causal, 0.75)
+    check_weights(weights, want, before)
+
+
+@pytest.mark.parametrize("d,tokens", [(64, 1), (128, 4), (128, 16), (256, 8)])
+def test_many_keys_with_gaps_and_nan(lib, d, tokens):
+    """Pages that are not there, NaN blocks behind the end and at a place that the last query alone sees."""
+    x = attention_inputs(lib, [tokens], [600], 16, 4, d, 16, BF)
+    x["table"][0, 2], x["table"][0, 20], x["table"][0, 21] = -1, 10 ** 6, -5
+    want = wanted(x)
+    clean = attend(lib, widened(x, 64, 8192), max_tokens=tokens)
+    check_attention(x, clean, want)
+    c, row, total = x["cache"], host(x["table"])[0], 600 + tokens
+    own = (row[(total - 1) // 16], (total - 1) % 16)
+    c.v_scales[own[0], own[1], 1, 0] = 255
+    for j in range(total, -(-total // 16) * 16):
+        c.v_scales[row[j // 16], j % 16] = 255
+        c.k_scales[row[j // 16], j % 16] = 255
+    out, lse = attend(lib, widened(x, 64, 8192), max_tokens=tokens)
+    nan = torch.zeros_like(out, dtype=torch.bool)
+    nan[tokens - 1, 4:8, :32] = True
+    assert torch.equal(out.isnan(), nan) and torch.equal(out[~nan], clean[0][~nan]) and torch.equal(lse, clean[1])
+
+
+# ---- offsets past 32 bits, streams, graphs -----------------------------------------------------------------------
+
+def far_cache(lib, x, pages):
+    """The same cache at the other end of a large one: page p is page pages - 1 - p. -> x with it"""
+    c = x["cache"]
+    big = [torch.empty(pages, *t.shape[1:], dtype=torch.uint8, device="cuda") for t in c]
+    for t, b in zip(c, big):
+        b[pages - t.shape[0]:] = t.flip(0)
+    return dict(x, cache=lib.Cache4(*big), table=torch.where(x["table"] < 0, -1, pages - 1 - x["table"]).to(torch.int32))
+
+
+def test_offsets_past_32_bits(lib):
+    """Pages 5 GB into a cache, and queries as far apart: bit for bit what the same ones near the front give."""
+    pages = 600_000
+    for new, ctx, N, keys in (([5, 1, 16], [300, 90, 0], 3, 400), ([1, 2], [300, 700], 64, 8192), ([70], [40], 1, 200)):
+        print("far", new, flush=True)
+        near = widened(attention_inputs(lib, new, ctx, 32, 8, 128, 16, BF), N, keys)
+        far = far_cache(lib, near, pages)
+        T = near["q"].shape[0]
+        room = torch.empty(T, 1 << 26, dtype=BF, device="cuda")[:, :32 * 128].unflatten(1, (32, 128))
+        room.copy_(near["q"])
+        far["q"] = room
+        got = [attend(lib, x, max_tokens=max(new)) for x in (near, far)]
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        w = [torch.zeros(x["cache"].k.shape[0], 8, 16, device="cuda") for x in (near, far)]
+        for x, y in zip((near, far), w):
+            lib.key_weights(x["q"], got[0][1], x["cache"], x["table"], x["starts"], x["totals"], y, max_tokens=max(new))
+        torch.cuda.synchronize()
+        n = w[0].shape[0]
+        assert torch.equal(w[0], w[1][pages - n:].flip(0)) and not w[1][:pages - n].any()
+        del room, far, w
+    x = evict_inputs(lib, [500, 90], 8, 128, 16)
+    far = far_cache(lib, x, pages)
+    n = x["weights"].shape[0]
+    far["weights"] = torch.zeros(pages, 8, 16, device="cuda")
+    far["weights"][pages - n:] = x["weights"].flip(0)
+    far["queue"] = x["queue"].clone()
+    args = ("weights", "table", "totals", "pages", "queue", "cursor")
+    for y in (x, far):
+        lib.evict(y["cache"], *(y[k] for k in args), budget=77, sinks=3, recent=9)
+    q, k, v, slots, positions, cs, _, w = rope_inputs(lib, 40, 16, 8, 128, 128, BF)
+    slots = torch.arange(40, dtype=torch.int32, device="cuda") + 32
+    lib.qk_norm_rope4(q, k, v, slots, positions, cs, x["cache"], q_weight=w[0], k_weight=w[1])
+    there = (pages - 1 - slots // 16) * 16 + slots % 16
+    lib.qk_norm_rope4(q, k, v, there.to(torch.int32), positions, cs, far["cache"], q_weight=w[0], k_weight=w[1])
+    torch.cuda.synchronize()
+    for a, b in zip((*x["cache"], x["weights"]), (*far["cache"], far["weights"])):
+        assert torch.equal(a, b[pages - n:].flip(0))
+
+
+def step_inputs(lib, seed):
+    """One decoding step of three requests: what all four calls need, and where their results go."""
+    x = evict_inputs(lib, [300, 500, 70], 4, 128, 16, seed=seed)
+    new = [4, 1, 2]
+    T, starts = sum(new), [0, 4, 5, 7]
+    q, k, v, _, _, cs, _, w = rope_inputs(lib, T, 16, 4, 128, 128, BF, seed=seed)
+    total, table = host(x["totals"]), host(x["table"])
+    at = [(n, total[n] - new[n] + i) for n in range(3) for i in range(new[n])]
+    x.update(q=q, k=k, v=v, cs=cs, w=w, starts=i32(starts), slots=i32([table[n, j // 16] * 16 + j % 16 for n, j in at]),
+             positions=i32([j for _, j in at]), turned=torch.zeros(T, 16, 128, dtype=BF, device="cuda"),
+             out=torch.zeros(T, 16, 128, dtype=BF, device="cuda"), lse=torch.zeros(T, 16, device="cuda"),
+             made=lib.Eviction(i32([0] * 3), i32([[0, 0]] * 3), torch.zeros(3, dtype=torch.int64, device="cuda"), i32([0] * 3)))
+    x["ws"] = lib.window_attention4_workspace(x["turned"], x["cache"], x["table"], max_tokens=4)
+    x["ews"] = lib.evict_workspace(x["cache"], x["table"], budget=100)
+    x["start"] = [t.clone() for t in (*x["cache"], x["weights"], x["queue"])]
+    return x
+
+
+def reset(x):
+    for t, s in zip((*x["cache"], x["weights"], x["queue"]), x["start"]):
+        t.copy_(s)
+    for t in (x["turned"], x["out"], x["lse"], *x["made"]):
+        t.zero_()
+
+
+def run_step(lib, x):
+    lib.qk_norm_rope4(x["q"], x["k"], x["v"], x["slots"], x["positions"], x["cs"], x["cache"], q_weight=x["w"][0],
+                      k_weight=x["w"][1], out=x["turned"])
+    lib.window_attention4(x["turned"], x["cache"], x["table"], x["starts"], x["totals"], max_tokens=4, lse=x["lse"],
+                          out=x["out"], workspace=x["ws"])
+    lib.key_weights(x["turned"], x["lse"], x["cache"], x["table"], x["starts"], x["totals"], x["weights"], decay=0.9,
+                    max_tokens=4)
+    lib.evict(x["cache"], x["weights"], x["table"], x["totals"], x["pages"], x["queue"], x["cursor"], budget=100,
+              sinks=4, recent=16, out=x["made"], workspace=x["ews"])
+
+
+def results(x):
+    return [t.clone() for t in (*x["cache"], x["weights"], x["queue"], x["turned"], x["out"], x["lse"], *x["made"])]
+
+
+def test_steps_on_two_streams(lib):
+    steps = [step_inputs(lib, s) for s in (1, 2)]
+    want = []
+    for x in steps:
+        run_step(lib, x)
+        torch.cuda.synchronize()
+        want.append(results(x))
+    streams = [torch.cuda.Stream() for _ in steps]
+    for again in range(3):
+        for x, s in zip(steps, streams):
+            with torch.cuda.stream(s):
+                reset(x)
+                run_step(lib, x)
+        torch.cuda.synchronize()
+        for x, w in zip(steps, want):
+            assert all(map(torch.equal, results(x), w))
+
+
+def test_captured_steps(lib):
+    """Two graphs that share their workspaces, replayed in turn, with eager steps between."""
+    steps = [step_inputs(lib, s) for s in (3, 4)]
+    steps[1]["ws"], steps[1]["ews"] = steps[0]["ws"], steps[0]["ews"]
+    want, graphs = [], []
+    for x in steps:
+        run_step(lib, x)
+        torch.cuda.synchronize()
+        want.append(results(x))
+    for x in steps:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run_step(lib, x)
+        graphs.append(g)
+    for again in range(3):
+        for x in steps:
+            reset(x)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for x, w in zip(steps, want):
+            assert all(map(torch.equal, results(x), w)), again
+        reset(steps[again % 2])
+        run_step(lib, steps[again % 2])
+        torch.cuda.synchronize()
+        assert all(map(torch.equal, results(steps[again % 2]), want[again % 2]))
