@@ -603,15 +603,6 @@ __device__ __forceinline__ void queries4(const uint16_t* at, int d, u32x4_t (&q)
   }
 }
 
-// Workgroup b, which runs on XCD b % 8, as an item: the head groups of a request's chunk come one after the other on one
-// XCD, so that they find the lines that they share in its L2, and the chunks go round the XCDs.
-__device__ __forceinline__ int beside(int b, int items, int head_groups) {
-  const int whole = items / head_groups / 8 * 8 * head_groups;
-  if (b >= whole) return b;
-  const int q = b / 8;
-  return (q / head_groups * 8 + b % 8) * head_groups + q % head_groups;
-}
-
 // Which rows a tile of BM has: request n, its first row r0 and the end r1 of them, first token, position of the first
 // query. False where there are none.
 struct Rows4 {

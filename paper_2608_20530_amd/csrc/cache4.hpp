@@ -80,6 +80,15 @@ __device__ __forceinline__ float quad_max(float v) {
 __device__ __forceinline__ uint32_t bits32_from(int n) { return n <= 0 ? ~0u : n >= 32 ? 0 : ~0u << n; }
 __device__ __forceinline__ uint32_t bits32_below(int n) { return ~bits32_from(n); }
 
+// Workgroup b, which runs on XCD b % 8, as an item, where `together` items in a row share cache lines: they come one after
+// the other on one XCD, so that they find the lines in its L2, and what follows goes round the XCDs.
+__device__ __forceinline__ int beside(int b, int items, int together) {
+  const int whole = items / together / 8 * 8 * together;
+  if (b >= whole) return b;
+  const int q = b / 8;
+  return (q / together * 8 + b % 8) * together + q % together;
+}
+
 // ---- host ------------------------------------------------------------------------------------------
 inline bool stride4_ok(int64_t s) { return s % 16 == 0 && s < ((int64_t)1 << 40); }
 

@@ -507,6 +507,12 @@ EVICT_CASES = [
     ([1500] * 70, 1, 64, 32, 1400, 1499, 4, 100, "phd"),
     ([3000], 2, 128, 16, 2999, 2999, 1, 1, "hpd"),
     ([40000, 33000], 1, 32, 64, 20000, 20000, 3, 500, "phd"),  # more than a workgroup keeps
+    ([40000, 20000], 1, 32, 5, 9000, 9000, 3, 50, "phd"),
+    ([16000, 15001, 3000], 2, 64, 16, 2000, 2000, 4, 30, "hpd"),
+    ([1500, 300, 260] * 24, 4, 128, 16, 200, 250, 4, 20, "phd"),  # many requests and heads
+    ([901] * 70, 2, 96, 24, 77, 100, 5, 13, "kv"),
+    ([1300, 900] * 33, 2, 256, 16, 600, 700, 1, 1, "wide"),
+    ([700] * 130, 1, 64, 32, 699, 699, 0, 0, "hpd"),
 ]
 
 
