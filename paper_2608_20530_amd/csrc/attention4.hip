@@ -129,7 +129,7 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
   int64_t chunk, chunks;
   if (p.heads > 1) {
     // A workgroup's share of the time should be small, the partial results' too, which with more rows weigh more: 256 tokens
-    // 466 us with 64 tiles a chunk, 474 with 48, 494 with 84; 64 blocks 379 with 84, 407 with 64, 385 with 128
+    // 446 us with 64 tiles a chunk, 449 with 48, 480 with 84; 64 blocks 310 with 84, 319 with 64, 346 with 128
     chunk = (most * items + 1535) / 1536;
     const int64_t cap = p.BM <= 16 ? 64 : 84;
     chunk = chunk < 8 ? 8 : chunk > cap ? cap : chunk;
@@ -263,7 +263,7 @@ void launch_weights(Attn4Args a, int d, bool heads_together, hipStream_t stream)
       };
       const int64_t pairs = (int64_t)a.N * a.kv_heads;
       if constexpr (RING) {
-        // (nothing is joined, so chunks are short: 256 tokens 283 us with 16 tiles, 290 with 32, 305 with 64)
+        // (nothing is joined, so chunks are short: 256 tokens 270 us with 16 tiles, 272 with 24, 275 with 32)
         if (a.kv_heads % 4 == 0 && heads_together && pairs * most >= kManyTiles)
           return launch(Attn4Config<T, D, 1, 4, 1, 1, RING>(), pairs / 4, 16);
       }
