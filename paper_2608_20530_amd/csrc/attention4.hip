@@ -12,7 +12,10 @@
 namespace lilicorr {
 namespace {
 
-// Many keys in all: a workgroup's waves share key heads rather than keys
+// Many keys in all (cache heads times tiles of 32 keys): a workgroup's waves share key heads rather than keys, and copies of
+// whole lines. 256 requests of one token, a million such tiles: 445 us against 548 with shared keys, their weights 270
+// against 362; 64 blocks 307 against 318. With fewer the workgroups do not fill the chip: a call of some ten thousand 139 us
+// with shared keys, 185 with shared heads.
 constexpr int64_t kManyTiles = 65536;
 constexpr size_t kLeastBytes4 = 256;  // of a workspace
 // The longest sequences have so many tokens: lengths, windows and sinks past it say "without end"
@@ -122,10 +125,13 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
   p.ring = ring_fits(a.cache);
   p.spread = own <= p.BM;
   // key heads over the waves, where that still leaves every compute unit work
-  const int wide = p.BM <= 16 || (p.BM <= 32 && a.cache.d <= 128) ? 4 : p.BM <= 64 && (a.cache.d <= 128 || p.BM == 32) ? 2 : 1;
+  const bool low = a.cache.d <= 128;
+  const int wide = p.BM == 16 || (p.BM == 32 && low) ? 4 : p.BM == 32 || (p.BM == 64 && low) ? 2 : 1;
   const int64_t pairs = tiles * a.cache.heads;
-  p.heads = p.ring && wide > 1 && a.cache.heads % wide == 0 && heads_together(a.cache) && pairs * most >= kManyTiles ? wide : 1;
-  const int64_t items = pairs / p.heads, wk = p.heads > 1 ? 1 : p.BM <= 32 ? (p.BM == 32 && a.cache.d > 128 ? 2 : 4) : p.BM == 64 && a.cache.d <= 128 ? 2 : 1;
+  const bool together = p.ring && wide > 1 && a.cache.heads % wide == 0 && heads_together(a.cache);
+  p.heads = together && pairs * most >= kManyTiles ? wide : 1;
+  const int64_t items = pairs / p.heads;
+  const int wk = p.heads > 1 ? 1 : wide;  // (waves that share keys are as many)
   int64_t chunk, chunks;
   if (p.heads > 1) {
     // A workgroup's share of the time should be small, the partial results' too, which with more rows weigh more: 256 tokens
@@ -135,7 +141,9 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
     chunk = chunk < 8 ? 8 : chunk > cap ? cap : chunk;
     chunks = (most + chunk - 1) / chunk;
   } else {
-    const int64_t want = 768;
+    // workgroups that all run at once; more of them only make more to join (37 requests of up to 33 tokens behind a window 34.7
+    // us, 36.2 with 768, 42.2 with 384; one token 18.4 with 512 and 768, 19.6 with 384)
+    const int64_t want = 512;
     chunks = items >= want ? 1 : want / items;
     const int64_t fit = (most + 2 * wk - 1) / (2 * wk);
     if (chunks > fit) chunks = fit;
@@ -321,7 +329,8 @@ extern "C" lilicorr_status lilicorr_window_attention4(const lilicorr_attention4_
   if (!x.q || !x.out || !c.k || !c.v || !c.k_scales || !c.v_scales || !x.table || !x.starts || !x.totals || x.q == x.out)
     return LILICORR_ERR_INVALID_ARG;
   if (!aligned16(x.q) || !aligned16(x.out) || !aligned16(c.k) || !aligned16(c.v) || !aligned16(x.workspace) ||
-      !aligned4(x.lse) || !aligned4(c.k_scales) || !aligned4(c.v_scales) || !aligned4(x.table) || !aligned4(x.starts) || !aligned4(x.totals))
+      !aligned4(x.lse) || !aligned4(c.k_scales) || !aligned4(c.v_scales) || !aligned4(x.table) ||
+      !aligned4(x.starts) || !aligned4(x.totals))
     return LILICORR_ERR_ALIGNMENT;
   if (!x.workspace || x.workspace_bytes < p.bytes) return LILICORR_ERR_WORKSPACE;
   if (x.max_tokens == 0) return LILICORR_OK;
@@ -351,8 +360,8 @@ extern "C" lilicorr_status lilicorr_key_weights(const lilicorr_key_weights_args*
   if (x.tokens == 0) return LILICORR_OK;
   if (!x.q || !x.lse || !x.weights || !c.k || !c.k_scales || !x.table || !x.starts || !x.totals)
     return LILICORR_ERR_INVALID_ARG;
-  if (!aligned16(x.q) || !aligned16(c.k) || !aligned16(x.weights) || !aligned4(x.lse) || !aligned4(c.k_scales) || !aligned4(x.table) ||
-      !aligned4(x.starts) || !aligned4(x.totals))
+  if (!aligned16(x.q) || !aligned16(c.k) || !aligned16(x.weights) || !aligned4(x.lse) || !aligned4(c.k_scales) ||
+      !aligned4(x.table) || !aligned4(x.starts) || !aligned4(x.totals))
     return LILICORR_ERR_ALIGNMENT;
   if (x.max_tokens == 0) return LILICORR_OK;
   // what other waves still read must not lie where the weights do

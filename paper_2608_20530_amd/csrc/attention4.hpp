@@ -3,7 +3,8 @@
 //
 // A row is one query head of one token; the query heads of a key head are neighbours, so the rows of a request and key
 // head are its tokens' groups one after the other. A wave holds RT blocks of 16 rows and goes through tiles of 32
-// keys; no data passes through LDS until the waves that shared the keys join.
+// keys. Tiles come by way of LDS, in rings of copies that go on while a tile is used, where widths are powers of two and
+// pages multiples of 16 keys (Ring4, Shared4); elsewhere loads go to registers, a tile ahead.
 //
 // 16 x 16 x 32 matrix instructions. The order of the summed index is free as long as both operands have the same, so
 // each operand is what a lane can load at once. Lane l is c = l % 16 and g = l / 16.
@@ -82,9 +83,9 @@ struct Attn4Config {
   // Several key heads in a workgroup: one ring for all. Rows of one head (prefill) do better each with their own copies than
   // with a barrier a tile: 1966 us against 2095.
   static constexpr bool kShared = WK == 1 && WH > 1;
-  // Stages of a ring. Two are enough where a compute unit has three workgroups (16 rows: 468 us for 256 tokens, 478 with
-  // three, 475 with four).
-  static constexpr int NS = D <= 64 ? 4 : D <= 128 && RT > 1 ? 3 : 2;
+  // Stages of a ring. Two are enough where a compute unit has two workgroups or three (256 tokens 445 us, 463 with three; 64
+  // blocks 306, 311 with three).
+  static constexpr int NS = D <= 64 ? 4 : 2;
   static constexpr int kWaves = WH * WR * WK, kThreads = kWaves * kWave;
   static constexpr int BM = 16 * RT * WR;
   static constexpr int ND = D / 16;  // output products
@@ -649,6 +650,11 @@ __device__ __forceinline__ bool rows4(const Attn4Args& a, int tile, Rows4& r) {
   return true;
 }
 
+// What bounds it, with 32 heads over 8 of 128: 256 tokens (100 to 16100 keys each) 445 us with the join, 5.1 TB/s: HBM, 0.76 of a
+// plain read. 64 blocks of 16 tokens 306 us, 8192 tokens of prefill 1960 to 1990 (830 TFLOP/s, 0.62 of a library
+// product): a tile of 32 rows and keys is 512 cycles of matrix instructions and 150 to 190 others, most of them
+// conversions, powers and sums, and two waves of a SIMD overlap a third of them. One token over 32768 keys 18.4 us:
+// latency, 14 of it here (lengths, pages, first tiles, output) and 5 in the join.
 template <typename C>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kSimdWaves, C::kSimdWaves)))
 void attention4_kernel(Attn4Args a) {
@@ -1128,7 +1134,7 @@ __device__ __forceinline__ int64_t weight_at(const Attn4Args& a, int page, int h
 
 // Requests with at most 16 rows: a wave goes through tiles of 32 keys as in the attention. The scores stand the
 // other way round, S[row][key], so that a lane has four rows of one key and the sum over rows is three
-// additions and two exchanges.
+// additions and two exchanges. 256 requests of one token (32 heads over 8 of 128) 270 us: HBM, 4.7 TB/s.
 template <typename C>
 __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char attn4_smem[];
@@ -1286,7 +1292,8 @@ __global__ __launch_bounds__(C::kThreads) void key_weights_few_kernel(Attn4Args 
 // scores stand as in the attention, S^T[key][row], so that a row's logarithm is one register and the sum over rows waits for
 // the end. The workgroup's waves have the keys of WK neighbouring groups and WR shares of the rows. Rows and their
 // logarithms come 64 at a time by way of LDS: loads in the operands' layout have neighbouring lanes in different rows
-// and kept the address unit busy four times as long as the matrix cores (a prompt's last 1024 tokens 525 us).
+// and kept the address unit busy four times as long as the matrix cores (a prompt's last 1024 tokens 525 us, 345 now:
+// 784 TFLOP/s, matrix instructions 31% of the cycles and 20% of them beside the powers that the rest goes to).
 __device__ const uint32_t kZeros4[4] = {0, 0, 0, 0};  // what is copied past the width of the head
 
 template <typename C>

@@ -432,7 +432,8 @@ extern "C" lilicorr_status lilicorr_evict(const lilicorr_evict_args* args, hipSt
   if (!c.k || !c.v || !c.k_scales || !c.v_scales || !x.weights || !x.table || !x.totals || !x.pages || !x.queue ||
       !x.cursor || !x.totals_out || !x.pages_out || !x.evicted || !x.cursor_out)
     return LILICORR_ERR_INVALID_ARG;
-  if (!aligned16(c.k) || !aligned16(c.v) || !aligned4(c.k_scales) || !aligned4(c.v_scales) || !aligned16(x.weights) || !aligned16(x.workspace) || !aligned4(x.table) ||
+  if (!aligned16(c.k) || !aligned16(c.v) || !aligned4(c.k_scales) || !aligned4(c.v_scales) ||
+      !aligned16(x.weights) || !aligned16(x.workspace) || !aligned4(x.table) ||
       !aligned4(x.totals) || !aligned4(x.pages) || !aligned4(x.queue) || !aligned8(x.cursor) ||
       !aligned4(x.totals_out) || !aligned4(x.pages_out) || !aligned4(x.evicted) || !aligned8(x.cursor_out))
     return LILICORR_ERR_ALIGNMENT;

@@ -649,7 +649,8 @@ __global__ __launch_bounds__(kRopeThreads, FOUR ? 4 : 1) void qk_norm_rope_kerne
                                          norm_k ? a.k_weight + (mine ? po : 0) : nullptr,
                                          a.rot ? a.cos_sin + (int64_t)pos * a.rot + p0 : nullptr, r.partner, r.turned,
                                          r.upper, a.d, a.eps, a.rot, a.interleaved);
-      const int64_t to = page * a.page_stride + (int64_t)(slot - page * a.page_size) * a.token_stride + (int64_t)h * a.head_stride;
+      const int64_t to = page * a.page_stride + (int64_t)(slot - page * a.page_size) * a.token_stride +
+                         (int64_t)h * a.head_stride;
       if (mine && h < a.kv_heads) {
         *reinterpret_cast<uint32_t*>((unsigned char*)a.k_cache + to + l * 4) = y.w;
         if (l % 4 == 0) a.k_scales[to / 16 + l / 4] = (unsigned char)y.scale;
@@ -808,7 +809,8 @@ extern "C" lilicorr_status lilicorr_qk_norm_rope4(const lilicorr_qk_norm_rope4_a
   // q rows that are turned in place must be laid out as the output is
   if (x.q_out == x.q && x.tokens > 1 && x.q_stride != (int64_t)x.heads * c.d) return LILICORR_ERR_INVALID_ARG;
   if (!aligned16(x.q) || !aligned16(x.k) || !aligned16(x.v) || !aligned16(x.q_out) || !aligned16(c.k) ||
-      !aligned16(c.v) || !aligned4(c.k_scales) || !aligned4(c.v_scales) || !aligned16(x.cos_sin) || !aligned16(x.q_weight) || !aligned16(x.k_weight) ||
+      !aligned16(c.v) || !aligned4(c.k_scales) || !aligned4(c.v_scales) || !aligned16(x.cos_sin) ||
+      !aligned16(x.q_weight) || !aligned16(x.k_weight) ||
       !aligned4(x.slots) || !aligned4(x.positions))
     return LILICORR_ERR_ALIGNMENT;
   // what other waves still read must not lie where q_out does, nor q_out in the cache
