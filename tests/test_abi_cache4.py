@@ -55,7 +55,7 @@ def _cache():
 
 
 def _rope():
-    return _make(L.QkNormRope4Args, cache=_cache(), q_stride=512, k_stride=128, v_stride=128, tokens=3, max_positions=100,
+    return _make(L.QkNormRope4Args, cache=_cache(), q_stride=512, k_stride=128, v_stride=128, tokens=5, max_positions=100,
                  dtype=1, heads=8, rot=64, eps=1e-6)
 
 
@@ -103,11 +103,11 @@ def test_qk_norm_rope4_refuses_overlaps(lib):
     for cache_part, last in (("k", 10 * 1024 - 16), ("v", 10 * 1024 - 16), ("k_scales", 636), ("v_scales", 636)):
         at = getattr(x.cache, cache_part)
         for name in ("q", "k", "v", "q_out"):
-            size = 3072 if name in ("q", "q_out") else 768  # 3 tokens of 8 or 2 heads of 64, 2 bytes
+            size = 5120 if name in ("q", "q_out") else 1280  # 5 tokens of 8 or 2 heads of 64, 2 bytes
             for a in (at, at + last // 16 * 16, at - size + 16):
                 assert lib.lilicorr_qk_norm_rope4(ctypes.byref(_change(_rope(), {name: a})), None) == -1, (cache_part, name)
-    for name, size in (("q", 3072), ("k", 768), ("v", 768)):
-        for a in (x.q_out + 16, x.q_out - size + 16, x.q_out + 3072 - 16):
+    for name, size in (("q", 5120), ("k", 1280), ("v", 1280)):
+        for a in (x.q_out + 16, x.q_out - size + 16, x.q_out + 5120 - 16):
             assert lib.lilicorr_qk_norm_rope4(ctypes.byref(_change(_rope(), {name: a})), None) == -1
     assert lib.lilicorr_qk_norm_rope4(ctypes.byref(_change(_rope(), dict(q=x.q_out, q_stride=520))), None) == -1
 
