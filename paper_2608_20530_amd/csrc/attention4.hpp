@@ -651,7 +651,7 @@ __device__ __forceinline__ bool rows4(const Attn4Args& a, int tile, Rows4& r) {
 }
 
 // What bounds it, with 32 heads over 8 of 128: 256 tokens (100 to 16100 keys each) 445 us with the join, 5.1 TB/s: HBM, 0.76 of a
-// plain read. 64 blocks of 16 tokens 306 us, 8192 tokens of prefill 1960 to 1990 (830 TFLOP/s, 0.62 of a library
+// plain read. 64 blocks of 16 tokens 306 us, 8192 tokens of prefill 1930 (855 TFLOP/s, 0.64 of a library
 // product): a tile of 32 rows and keys is 512 cycles of matrix instructions and 150 to 190 others, most of them
 // conversions, powers and sums, and two waves of a SIMD overlap a third of them. One token over 32768 keys 18.4 us:
 // latency, 14 of it here (lengths, pages, first tiles, output) and 5 in the join.
@@ -719,13 +719,15 @@ void attention4_kernel(Attn4Args a) {
 
   f32x4_t o[C::RT][C::ND];
   float m[C::RT], l[C::RT], lu[C::RT];
+  f32x4_t ls[C::RT];
   uint32_t poison[C::RT];
 #pragma unroll
   for (int t = 0; t < C::RT; ++t) {
 #pragma unroll
     for (int i = 0; i < C::ND; ++i) o[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     m[t] = -__builtin_inff();
-    l[t] = lu[t] = 0.f;
+    lu[t] = 0.f;
+    ls[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     poison[t] = 0;
   }
 
@@ -784,7 +786,6 @@ void attention4_kernel(Attn4Args a) {
         e[x] = __builtin_amdgcn_exp2f(fmaf(sc[t][x / 4][x % 4], a.scale2, -ms));
         lu[t] += e[x];
       }
-      typedef __bf16 pair __attribute__((ext_vector_type(2)));
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const uint32_t w = Bf16::pack(e[2 * x], e[2 * x + 1]);
@@ -792,11 +793,14 @@ void attention4_kernel(Attn4Args a) {
         if constexpr (C::kTerms > 1) {
           const f32x2_t hi = Bf16::unpack(w);
           pf[t][1][x] = Bf16::pack(e[2 * x] - hi[0], e[2 * x + 1] - hi[1]);
-        } else {
-          l[t] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, 0x3f803f80u),
-                                                 l[t], false);
         }
       }
+    }
+    if constexpr (C::kTerms == 1) {
+      // sums of the rounded probabilities, in every register of a lane (prefill 1933 us, 1985 with vector instructions)
+      const u32x4_t ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+      for (int t = 0; t < C::RT; ++t) ls[t] = mfma16(ones, pf[t][0], ls[t]);
     }
     if (!whole) {  // NaN blocks of values
       uint32_t top = 0;
@@ -862,8 +866,8 @@ void attention4_kernel(Attn4Args a) {
       // nothing is accumulated while m is -inf
       const float f = grows ? __builtin_amdgcn_ldexpf(1.f, (int)fmaxf(m[t] - to, -300.f)) : 1.f;
       m[t] = grows ? to : m[t];
-      l[t] *= f;
       lu[t] *= f;
+      ls[t] *= f;
 #pragma unroll
       for (int i = 0; i < C::ND; ++i)
 #pragma unroll
@@ -975,7 +979,7 @@ void attention4_kernel(Attn4Args a) {
 #pragma unroll
   for (int t = 0; t < C::RT; ++t) {
     lu[t] = quad_sum(lu[t]);
-    l[t] = C::kTerms > 1 ? lu[t] : quad_sum(l[t]);  // two terms of a probability round next to nothing
+    l[t] = C::kTerms > 1 ? lu[t] : ls[t][0];  // two terms of a probability round next to nothing
     if (__ballot(poison[t] != 0)) {
       // lane (c, g) has the elements D / 4 g + D / 16 r + i of its row, in o[t][i][r]
 #pragma unroll
