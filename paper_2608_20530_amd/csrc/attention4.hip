@@ -30,6 +30,10 @@ struct Plan4 {
   size_t bytes;  // of the workspace
 };
 
+// Whether a wave has registers for two blocks of 16 rows: tiles by way of registers leave wider heads none (2048 tokens behind
+// 2048, heads of 96: 606 us with two blocks, whose registers spill, 285 with one).
+constexpr bool two_blocks4(int d, bool ring) { return d <= (ring ? 128 : 64); }
+
 // Calls `use` with the kernel of a width, a tile height and what the workgroup's waves share: key heads (`heads`: a token's
 // heads lie side by side, and so share cache lines) or keys.
 template <typename T, int D, bool RING, typename F>
@@ -46,7 +50,7 @@ void with_rows4(int BM, bool heads, const F& use) {
     }
   }
   if (BM == 16) return use(Attn4Config<T, D, 1, 1, 1, 4, RING>());
-  if constexpr (D > 128) {
+  if constexpr (!two_blocks4(D, RING)) {
     if (BM == 32) return use(Attn4Config<T, D, 1, 1, 2, 2, RING>());
     return use(Attn4Config<T, D, 1, 1, 4, 1, RING>());
   } else {
@@ -55,7 +59,7 @@ void with_rows4(int BM, bool heads, const F& use) {
     return use(Attn4Config<T, D, 2, 1, 4, 1, RING>());
   }
 }
-int tile_rows4(int64_t rows, int d) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || d > 128 ? 64 : 128; }
+int tile_rows4(int64_t rows, bool two) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || !two ? 64 : 128; }
 
 template <typename T, typename F>
 void with_kernel4(int d, bool ring, int BM, bool heads, const F& use) {
@@ -108,7 +112,9 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
   const int64_t max_tokens = a.max_tokens < a.tokens ? a.max_tokens : a.tokens;
   p.rows = a.tokens * a.heads;
   const int64_t own = max_tokens * group;
-  p.BM = tile_rows4(own, a.cache.d);
+  p.ring = ring_fits(a.cache);
+  const bool two = two_blocks4(a.cache.d, p.ring);
+  p.BM = tile_rows4(own, two);
   const int64_t tiles = own <= p.BM ? a.N : a.tokens * group / p.BM + a.N;
   int64_t keys = a.table_width * a.cache.page_size;
   if (a.max_length < keys) keys = a.max_length;
@@ -122,11 +128,9 @@ lilicorr_status make_plan4(const lilicorr_attention4_args& a, Plan4& p) {
     if (tiles32 < most) most = tiles32;
   }
   if (most < 1) most = 1;
-  p.ring = ring_fits(a.cache);
   p.spread = own <= p.BM;
   // key heads over the waves, where that still leaves every compute unit work
-  const bool low = a.cache.d <= 128;
-  const int wide = p.BM == 16 || (p.BM == 32 && low) ? 4 : p.BM == 32 || (p.BM == 64 && low) ? 2 : 1;
+  const int wide = p.BM == 16 || (p.BM == 32 && two) ? 4 : p.BM == 32 || (p.BM == 64 && two) ? 2 : 1;
   const int64_t pairs = tiles * a.cache.heads;
   const bool together = p.ring && wide > 1 && a.cache.heads % wide == 0 && heads_together(a.cache);
   p.heads = together && pairs * most >= kManyTiles ? wide : 1;

@@ -96,10 +96,12 @@ struct Attn4Config {
   // the waves' partial outputs, in the order of their lanes, and sums
   static constexpr uint32_t kOut = kWaves * RT * ND * kWave * 16, kSums = kWaves * RT * kWave * 16;
   static constexpr uint32_t kJoin = WK > 1 ? kOut + kSums : 0;
-  // waves of a SIMD that the registers are given out for: two or more keep the accumulators where the vector unit
-  // reaches them
-  static constexpr int kSimdWaves =
-      D > 128 || (RT == 2 && D > 64 && kTerms > 1) ? 1 : RT == 1 && kTerms == 1 ? 3 : 2;
+  // Waves of a SIMD that the registers are given out for: two or more keep the accumulators where the vector unit reaches
+  // them. Tiles by way of registers need more of those: with three waves they spill (64 requests of one token, heads of
+  // 96: 463 us, 98 with two).
+  static constexpr int kSimdWaves = D > 128 || (RT == 2 && D > 64 && kTerms > 1)         ? 1
+                                    : RT == 1 && kTerms == 1 && (RING || D <= 64) ? 3
+                                                                                         : 2;
 };
 
 // What a wave has under way of a tile of 32 keys
