@@ -296,6 +296,10 @@ ATTENTION_CASES = [
     ([1] * 70, list(range(70)), 4, 2, 64, 16, 0, 0, True, BF),
     ([1, 90] * 20, list(range(40)), 2, 1, 64, 16, 33, 2, True, HF),
     ([4, 8], [900, 40], 8, 2, 128, 48, 200, 40, True, BF),
+    ([8, 3], [300, 70], 8, 2, 128, 24, 0, 0, True, BF),  # pages and widths that go by way of registers
+    ([16, 1], [200, 41], 8, 2, 96, 16, 0, 0, True, HF),
+    ([60, 25], [100, 300], 8, 2, 128, 24, 77, 5, False, HF),
+    ([90], [150], 4, 2, 96, 32, 0, 0, True, BF),
 ]
 
 
