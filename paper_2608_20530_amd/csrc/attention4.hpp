@@ -39,8 +39,6 @@ namespace {
 
 typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4_t;
 
-constexpr float kRescale4 = 8.f;  // growth of the maximum, in powers of two, that is let pass
-
 // the largest of three; a NaN counts only beside NaNs
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
@@ -734,10 +732,11 @@ void attention4_kernel(Attn4Args a) {
   }
 
   // One tile, whose keys all rows see (`whole`) or not: `here` are those that there are. False, and nothing accumulated,
-  // where a maximum has grown too far over its reference: then grow(), and again. The accumulators change
-  // outside the loop over the tiles, since the compiler copies them at every join of paths inside it (38 moves a tile with
-  // two blocks of rows, 144 with four).
+  // where a maximum has grown too far over its reference: then grow(), and again, twice at most (where one
+  // row's reference goes far, the others' products are rounded too, which may find another a little grown). The accumulators change outside the loop over the tiles, since the compiler copies them
+  // at every join of paths inside it (38 moves a tile with two blocks of rows, 144 with four).
   float mx[C::RT];
+  uint64_t far = 0;  // which lanes' references are far
   auto step = [&](Raw4<C>& r, int j0, uint32_t here, bool whole) __attribute__((always_inline)) -> bool {
     uint32_t vis[C::RT];
     if (!whole) {
@@ -775,8 +774,18 @@ void attention4_kernel(Attn4Args a) {
       mx[t] = max3(mx[t], sc[t][0][3], sc[t][1][0]);
       mx[t] = max3(mx[t], sc[t][1][1], sc[t][1][2]);
       mx[t] = max3(mx[t], sc[t][1][3], mx[t]);
-      up |= fmaf(mx[t], a.scale2, -m[t]) > kRescale4;  // -inf - -inf is NaN and does not count
     }
+    const float s2 = far ? 1.f : a.scale2;  // what scores have still to be multiplied by
+    if (__builtin_expect(far != 0, 0)) {
+#pragma unroll
+      for (int t = 0; t < C::RT; ++t) {
+        mx[t] = scaled4(mx[t], a.scale2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sc[t][e / 4][e % 4] = scaled4(sc[t][e / 4][e % 4], a.scale2);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < C::RT; ++t) up |= grown4(mx[t], s2, m[t]);
     if (__builtin_expect(__ballot(up) != 0, 0)) return false;
     u32x4_t pf[C::RT][C::kTerms];
 #pragma unroll
@@ -785,7 +794,7 @@ void attention4_kernel(Attn4Args a) {
       float e[8];
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
-        e[x] = __builtin_amdgcn_exp2f(fmaf(sc[t][x / 4][x % 4], a.scale2, -ms));
+        e[x] = __builtin_amdgcn_exp2f(fmaf(sc[t][x / 4][x % 4], s2, -ms));
         lu[t] += e[x];
       }
 #pragma unroll
@@ -860,14 +869,16 @@ void attention4_kernel(Attn4Args a) {
     return true;
   };
   auto grow = [&]() __attribute__((always_inline)) {
+    const float s2 = far ? 1.f : a.scale2;
 #pragma unroll
     for (int t = 0; t < C::RT; ++t) {
       const float top = quad_max(mx[t]);
-      const bool grows = fmaf(top, a.scale2, -m[t]) > kRescale4;
-      const float to = __builtin_floorf(top * a.scale2);
+      const bool grows = grown4(top, s2, m[t]);
+      const float to = reference4(top, s2);
       // nothing is accumulated while m is -inf
       const float f = grows ? __builtin_amdgcn_ldexpf(1.f, (int)fmaxf(m[t] - to, -300.f)) : 1.f;
       m[t] = grows ? to : m[t];
+      far |= __ballot(far4(m[t]));
       lu[t] *= f;
       ls[t] *= f;
 #pragma unroll

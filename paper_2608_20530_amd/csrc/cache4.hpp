@@ -7,6 +7,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "common.hpp"
@@ -75,6 +76,24 @@ __device__ __forceinline__ float quad_max(float v) {
   const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+
+// The reference m of a row's powers 2^(x s - m), x a score and s the scale: a whole number that follows the largest score
+// when that has grown by more than 2^8, and -inf before the first one. A tile in which one has grown is done again after the
+// growth, so a growth has to end that whatever the score. In the difference the product x s is not rounded, and where m
+// comes from it it is: up to 2^24 the two are less than two apart, from 2^28 on rounding alone can make up more
+// than 2^8, for good. So from 2^24 on (`far4`) scores are multiplied and rounded first, as m was, and then s is 1.
+constexpr float kRescale4 = 8.f;
+constexpr float kFar4 = 0x1p24f;
+__host__ __device__ inline float scaled4(float x, float s) {
+#pragma clang fp contract(off)
+  return x * s;
+}
+__host__ __device__ inline bool grown4(float x, float s, float m) {
+  return fmaf(x, s, -m) > kRescale4;  // -inf - -inf is NaN and does not count
+}
+// (finite below, where -inf would stay -inf)
+__host__ __device__ inline float reference4(float x, float s) { return floorf(fmaxf(scaled4(x, s), -__FLT_MAX__)); }
+__host__ __device__ inline bool far4(float m) { return fabsf(m) >= kFar4 && m != -__builtin_inff(); }
 
 // bits at and above n, and below it, of 32 (any n)
 __device__ __forceinline__ uint32_t bits32_from(int n) { return n <= 0 ? ~0u : n >= 32 ? 0 : ~0u << n; }
