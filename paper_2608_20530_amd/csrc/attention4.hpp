@@ -39,11 +39,10 @@ namespace {
 
 typedef __attribute__((address_space(3))) f32x4_t* lds_f32x4_t;
 
-// the largest of three; a NaN counts only beside NaNs
+// the largest of three, NaN if one of them is (a row that sees one is NaN anyway). As operations that the compiler
+// knows: it puts no wait between a matrix instruction and inline assembly that reads its result.
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  __asm__("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
 struct Attn4Args {
