@@ -88,11 +88,10 @@ __device__ __forceinline__ float add_pair<F16>(uint32_t w, float c) {
   return __builtin_amdgcn_fdot2(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, 0x3c003c00u), c, false);
 }
 
-// the largest of three; a NaN counts only beside NaNs
+// the largest of three, NaN if one of them is (a row that sees one is NaN anyway). As operations that the compiler
+// knows: it puts no wait between a matrix instruction and inline assembly that reads its result.
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  __asm__("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
 // bits at and above n, and below it, of 64 (any n)
