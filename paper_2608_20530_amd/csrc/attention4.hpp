@@ -1088,6 +1088,11 @@ __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Arg
   const int x = (lane % LPR) * 4;
   if (row >= a.rows) return;
   const int64_t used = (int64_t)min(max(a.starts[a.N], 0), a.tokens) * a.heads;
+  // Whether this lane's slot of turn (b, u) saw anything. The uniform part of its number is shifted by the scalar unit: a
+  // 64-bit vector shift by a lane's own amount went wrong where the amount lay in the wave's last register.
+  auto saw_of = [&](uint64_t which, int b, int u) {
+    return (uint32_t)(which >> (b + u * kAtOnce)) >> (lane / LPR) & 1;
+  };
   float top = -__builtin_inff(), l = 0.f, lu = 0.f;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < slots; s0 += kWave) {
@@ -1099,7 +1104,7 @@ __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Arg
       for (int u = 0; u < kBatch; ++u) {
         const int s = b + u * kAtOnce + lane / LPR;
         v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (s < here && x < a.d && (FEW || (which >> (s & 63) & 1)))
+        if (s < here && x < a.d && (FEW || saw_of(which, b, u)))
           v[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + ((s0 + s) * a.rows + row) * a.d + x);
       }
     };
@@ -1121,7 +1126,7 @@ __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Arg
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         const int s = b + u * kAtOnce + lane / LPR;
-        const bool on = s < here && ((which >> (s & 63)) & 1);
+        const bool on = s < here && saw_of(which, b, u);
         const float w = __shfl(f, s & 63, kWave);
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += on ? w * v[u][e] : 0.f;

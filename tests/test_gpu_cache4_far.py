@@ -16,11 +16,11 @@ CASES = [
     ([1], [700], 8, 2, 128, 16, BF, 1, 720),
     ([16], [300], 8, 2, 64, 16, HF, 1, 400),
     ([90], [50], 4, 1, 128, 16, BF, 1, 160),
-    ([7], [90], 4, 2, 256, 16, BF, 1, 112),
+    ([7], [90], 4, 2, 256, 16, BF, 1, 128),
     ([1], [900], 16, 4, 128, 16, BF, 64, 8192),
     ([16], [500], 16, 4, 128, 16, HF, 64, 8192),
-    ([8], [300], 8, 2, 128, 24, HF, 1, 320),
-    ([40], [70], 6, 2, 96, 16, BF, 1, 112),
+    ([8], [300], 8, 2, 128, 24, HF, 1, 336),
+    ([40], [70], 6, 2, 96, 16, BF, 1, 128),
 ]
 
 
