@@ -270,12 +270,14 @@ struct RopeLane {
   bool turned, upper;   // whether this lane's elements turn; whether they are the pairs' b
 };
 
-// y: the lane's eight elements; `size` (BOUND) for each the sum of the magnitudes that it was made from
+// y: the lane's eight elements. BOUND: `size` for each the sum of the magnitudes that it was made from, `sound` whether
+// the mean of squares lies where fp32 neither overflows nor gets coarse
 template <typename T, int LPH, bool BOUND>
 __device__ __forceinline__ void norm_turn32(const u32x4_t& w, bool norm, const float (&wt)[8],
                                             const float (&wp)[8], const RopeLane& r, int d, float eps, int rot,
-                                            int interleaved, float (&y)[8], float (&size)[8]) {
+                                            int interleaved, float (&y)[8], float (&size)[8], bool& sound) {
   float x[8];
+  sound = true;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const f32x2_t t = T::unpack(w[i]);
@@ -288,7 +290,9 @@ __device__ __forceinline__ void norm_turn32(const u32x4_t& w, bool norm, const f
 #pragma unroll
     for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
     s = head_sum<LPH>(s);
-    inv = rsqrtf(s * (1.f / (float)d) + eps);
+    const float mean = s * (1.f / (float)d) + eps;
+    if constexpr (BOUND) sound = mean > 0x1p-60f && mean < 0x1p60f;
+    inv = rsqrtf(mean);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = norm ? x[i] * inv * wt[i] : x[i];
@@ -335,8 +339,9 @@ template <typename T, int LPH>
 __device__ __forceinline__ u32x4_t norm_turn(const u32x4_t& w, bool norm, const float (&wt)[8],
                                              const float (&wp)[8], const RopeLane& r, int d,
                                              float eps, int rot, int interleaved) {
-  float y[8], none[8];
-  norm_turn32<T, LPH, false>(w, norm, wt, wp, r, d, eps, rot, interleaved, y, none);
+  float y[8], size[8];
+  bool sound;
+  norm_turn32<T, LPH, false>(w, norm, wt, wp, r, d, eps, rot, interleaved, y, size, sound);
   u32x4_t out;
 #pragma unroll
   for (int i = 0; i < 4; ++i) out[i] = T::pack(y[2 * i], y[2 * i + 1]);
@@ -487,21 +492,26 @@ __device__ __forceinline__ Code4 quantise64(const u32x4_t& w, const float* weigh
 // A key in fp32, and whether some element's scale, code or sign is not certain: then it is done again in 64 bits. An
 // element is at most 2^-20 of the magnitudes that it was made from off (sum of squares 13 roundings, halved by the
 // root; mean, root, two factors, two products and a sum: 16 in all of 2^-24), so it is certain where four times that
-// up or down changes nothing. With normal values one step of a wave in 400 is done again.
-constexpr float kUncertain = 0x1p-18f;
+// up or down changes nothing. That holds where nothing overflows (the size is infinite or the mean too large then) and
+// where what underflows does not count: with a mean of 2^-60 .. 2^60 and weights up to kWild a product that fp32 rounds more
+// coarsely than 2^-24 makes an error of 2^-129 in the end, which is nothing beside an element over kSmall; one below is done
+// again unless it is 0 and comes from 0. With normal values one step of a wave in 400 is done again.
+constexpr float kUncertain = 0x1p-18f, kSmall = 0x1p-110f, kWild = 0x1p20f;
 template <typename T, int LPH>
 __device__ __forceinline__ Code4 quantise_key(const u32x4_t& w, bool norm, const float (&wt)[8], const float (&wp)[8],
                                               const RopeLane& r, int d, float eps, int rot, int interleaved,
                                               bool& unsure) {
   float y[8], size[8], lo[8], hi[8], most_lo = 0.f, most_hi = 0.f;
-  norm_turn32<T, LPH, true>(w, norm, wt, wp, r, d, eps, rot, interleaved, y, size);
-  unsure = false;
+  bool sound;
+  norm_turn32<T, LPH, true>(w, norm, wt, wp, r, d, eps, rot, interleaved, y, size, sound);
+  unsure = !sound;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float off = size[i] * kUncertain, v = fabsf(y[i]);
     lo[i] = v - off;
     hi[i] = v + off;
-    unsure |= !(lo[i] > 0.f) && size[i] != 0.f;  // the sign; NaN
+    const uint32_t word = w[i / 2];
+    unsure |= !(lo[i] > kSmall) && fabsf(T::unpack(word)[i % 2]) != size[i];  // (0 of 0 is certain) the sign; NaN
     most_lo = fmaxf(most_lo, lo[i]);
     most_hi = fmaxf(most_hi, hi[i]);
   }
@@ -538,6 +548,10 @@ __global__ __launch_bounds__(kRopeThreads, FOUR ? 4 : 1) void qk_norm_rope_kerne
     load_floats<8>(a.k_weight + (mine ? e0 : 0), kw);
     load_floats<8>(a.k_weight + (mine ? po : 0), kp);
   }
+  bool wild = false;
+  if (FOUR && norm_k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) wild |= !(fabsf(kw[i]) <= kWild);
 
   const int qs = (a.heads + kHeads - 1) / kHeads, ks = (a.kv_heads + kHeads - 1) / kHeads;
   const int steps = qs + 2 * ks;
@@ -550,7 +564,7 @@ __global__ __launch_bounds__(kRopeThreads, FOUR ? 4 : 1) void qk_norm_rope_kerne
   // 119 us for 16381 tokens).
   constexpr int kAgain = 64;
   __shared__ uint32_t s_again[FOUR ? kRopeThreads / kWave : 1][FOUR ? kAgain : 1];
-  uint32_t again = 0, turn = 0;
+  uint32_t again = __ballot(wild) ? kAgain + 1 : 0, turn = 0;
   for (int64_t it = (int64_t)blockIdx.x * (kRopeThreads / kWave) + wave; it < items; it += waves, ++turn) {
     const int64_t t = it / a.parts;
     const int part = (int)(it - t * a.parts);
