@@ -367,10 +367,12 @@ __device__ __forceinline__ uint32_t codes4(const float (&y)[8], float scale) {
   return w;
 }
 
-// the largest over four neighbouring lanes
+// the largest over four neighbouring lanes, NaN if one is
 __device__ __forceinline__ float block_max(float v) {
-  v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, false)));
-  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, false)));
+  v = __builtin_elementwise_maximum(
+      v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, false)));
+  return __builtin_elementwise_maximum(
+      v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, false)));
 }
 
 struct Code4 {
@@ -494,9 +496,10 @@ __device__ __forceinline__ Code4 quantise64(const u32x4_t& w, const float* weigh
 // root; mean, root, two factors, two products and a sum: 16 in all of 2^-24), so it is certain where four times that
 // up or down changes nothing. That holds where nothing overflows (the size is infinite or the mean too large then) and
 // where what underflows does not count: with a mean of 2^-60 .. 2^60 and weights up to kWild a product that fp32 rounds more
-// coarsely than 2^-24 makes an error of 2^-129 in the end, which is nothing beside an element over kSmall; one below is done
-// again unless it is 0 and comes from 0. With normal values one step of a wave in 400 is done again.
-constexpr float kUncertain = 0x1p-18f, kSmall = 0x1p-110f, kWild = 0x1p20f;
+// coarsely than 2^-24 makes an error of 2^-129 in the end and a pair below 2^-105. An element that is not over kSmall is done
+// again unless its own x is 0 (the other of its pair sees to what that one makes). With normal values one step of a wave
+// in 400 is done again.
+constexpr float kUncertain = 0x1p-18f, kSmall = 0x1p-100f, kWild = 0x1p20f;
 template <typename T, int LPH>
 __device__ __forceinline__ Code4 quantise_key(const u32x4_t& w, bool norm, const float (&wt)[8], const float (&wp)[8],
                                               const RopeLane& r, int d, float eps, int rot, int interleaved,
@@ -511,9 +514,9 @@ __device__ __forceinline__ Code4 quantise_key(const u32x4_t& w, bool norm, const
     lo[i] = v - off;
     hi[i] = v + off;
     const uint32_t word = w[i / 2];
-    unsure |= !(lo[i] > kSmall) && fabsf(T::unpack(word)[i % 2]) != size[i];  // (0 of 0 is certain) the sign; NaN
+    unsure |= !(lo[i] > kSmall) && T::unpack(word)[i % 2] != 0.f;  // the sign
     most_lo = fmaxf(most_lo, lo[i]);
-    most_hi = fmaxf(most_hi, hi[i]);
+    most_hi = __builtin_elementwise_maximum(most_hi, hi[i]);  // NaN if one is
   }
   most_lo = block_max(most_lo);
   most_hi = block_max(most_hi);
