@@ -108,6 +108,9 @@ __device__ __forceinline__ int beside(int b, int items, int together) {
   return (q / together * 8 + b % 8) * together + q % together;
 }
 
+// How many of a thread's loads of page numbers, and then of weights, the eviction has under way at a time
+constexpr int loads_at_once(int slots) { return slots < 8 ? slots : 8; }
+
 // ---- host ------------------------------------------------------------------------------------------
 inline bool stride4_ok(int64_t s) { return s % 16 == 0 && s < ((int64_t)1 << 40); }
 

@@ -128,13 +128,13 @@ __global__ __launch_bounds__(kSelectThreads, G == 4 && KEYS == 16 ? 8 : 4) void 
   const int stretches = (int)uniform32((row.length + kStretch - 1) / kStretch);
   const int per = stretches > 1 ? kKeys : ((row.length + kSelectThreads - 1) / kSelectThreads + 3) / 4 * 4;
   // The weights' order, greater for the heavier (a token without a page comes last), and slots of the first of G tokens.
-  // Eight loads under way at a time, pages and then weights.
+  constexpr int kSlots = kKeys / G, kAtOnce = loads_at_once(kSlots);
+  static_assert(kKeys % G == 0 && kSlots % kAtOnce == 0, "batches fill the arrays");
   uint32_t key[kKeys] = {};
-  int slot[kKeys / G];
+  int slot[kSlots];
   auto read = [&](int jt) {
-    constexpr int kAtOnce = 8;
 #pragma unroll
-    for (int x0 = 0; x0 < kKeys / G; x0 += kAtOnce) {
+    for (int x0 = 0; x0 < kSlots; x0 += kAtOnce) {
       if (x0 * G >= per) break;
       int page[kAtOnce], o[kAtOnce];
 #pragma unroll
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kSelectThreads, G == 4 && KEYS == 16 ? 8 : 4) void 
     int e0 = base_equal + (int)(sum >> 16);
     int at = base_more + (int)(sum & 0xffff) + min(e0, need);
 #pragma unroll
-    for (int x = 0; x < kKeys / G; ++x)
+    for (int x = 0; x < kSlots; ++x)
 #pragma unroll
       for (int y = 0; y < G; ++y) {
         const int i = x * G + y;
