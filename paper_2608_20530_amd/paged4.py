@@ -148,6 +148,8 @@ def _part(codes, scales, name: str, shape: tuple, strides: tuple) -> tuple:
 
 def _cache(c: Cache4, values: bool = True) -> tuple:
     """The fields of Cache4Args."""
+    if c.k is None or c.k_scales is None or (values and (c.v is None or c.v_scales is None)):
+        raise LilicorrError(f"this call needs the cache's keys{' and values' if values else ''}, codes and scales")
     shape, strides = c.k.shape, c.k.stride()
     k, ks = _part(c.k, c.k_scales, "keys", shape, strides)
     v, vs = _part(c.v, c.v_scales, "values", shape, strides) if values else (0, 0)
