@@ -8,7 +8,7 @@ host synchronisation:
   page_plan          where the step's tokens go
   qk_norm_rope4      queries and keys normed and rotated, keys and values into the cache in 4 bits
   window_attention4  the block against its request's keys, and each row's log of its sum of exponentials
-  key_weights        how much of its attention every key has got so far
+  key_weights        how much of its attention every key has got so far, from the tokens that were accepted
   evict              requests past their limit cut to the budget, their last pages back to the queue
   topk, score_walk   the block's logits to the next draft
 
@@ -59,9 +59,10 @@ class BudgetLayer:
         y = (x @ self.w_qkv).view(x.shape[0], self.heads + 2 * self.kv, self.d)
         return y.split((self.heads, self.kv, self.kv), 1)
 
-    def step(self, x, incoming, tokens, most):
+    def step(self, x, incoming, tokens, most, weigh=True):
         """x [tokens, hidden], request by request; incoming [N] int32 on the device (negative: the
-        request ends). tokens and most (of one request) are what the host knows. -> [tokens, hidden]"""
+        request ends). tokens and most (of one request) are what the host knows. Without `weigh` the keys' weights wait
+        for a call of weigh(), when it is known which tokens stay. -> [tokens, hidden]"""
         plan = L.page_plan(self.lengths, incoming, self.pages, self.table, self.queue, self.cursor,
                            page_size=self.page_size, tokens=tokens)
         self.pages, self.cursor, self.lengths = plan.pages, plan.cursor, plan.totals
@@ -77,8 +78,18 @@ class BudgetLayer:
         bounds = dict(max_tokens=most, max_length=self.longest)
         lse = torch.empty(tokens, self.heads, device="cuda")
         o = L.window_attention4(q, self.cache, self.table, plan.starts, plan.totals, lse=lse, **bounds)
-        L.key_weights(q, lse, self.cache, self.table, plan.starts, plan.totals, self.weights, decay=self.decay, **bounds)
+        self.open = (q, lse, plan, row - plan.starts[request], request, bounds)
+        if weigh:
+            self.weigh()
         return o.flatten(1) @ self.w_out
+
+    def weigh(self, accepted=None):
+        """Adds what the last step's queries gave to every key; with `accepted` [N] of each request's first tokens alone
+        (a row whose logarithm is -inf adds nothing). Before the lengths change."""
+        q, lse, plan, token, request, bounds = self.open
+        if accepted is not None:
+            lse = lse.masked_fill((token >= accepted[request])[:, None], -torch.inf)
+        L.key_weights(q, lse, self.cache, self.table, plan.starts, plan.totals, self.weights, decay=self.decay, **bounds)
 
     def cut(self):
         """Requests past their limit keep their budget."""
@@ -109,12 +120,13 @@ def serve(steps=12, N=8, B=16, K=8, V=32000, hidden=256, prompt=300, budget=128,
     block = torch.full((N,), B, dtype=torch.int32, device="cuda")
     drafts = []
     for s in range(steps):
-        y = layer.step(embed(draft), block, N * B, B)
+        y = layer.step(embed(draft), block, N * B, B, weigh=False)
         logits = (y @ E.T).view(N, B, V)
         ids, logp = L.topk(logits, K)
         draft, _, _ = L.score_walk(ids, logp, E, packed)
         drafts.append(draft)
         accepted = torch.randint(1, B + 1, (N,), generator=g, device="cuda", dtype=torch.int32)
+        layer.weigh(accepted)  # what rejected tokens looked at counts for nothing
         # from the step's totals: a request whose pages ran out is shorter than its last one's says
         layer.keep(layer.lengths - (B - accepted))
         layer.cut()

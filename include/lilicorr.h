@@ -711,6 +711,8 @@ lilicorr_status lilicorr_window_attention4(const lilicorr_attention4_args *args,
  * where before is weights[j][h] for the keys j < totals[n] - T of earlier steps and 0 for the step's own keys (so that a
  * page needs no clearing when it changes hands). Without a window: query t sees keys up to its own when
  * `causal`, else all. Requests without queries, and keys on pages that are not there, are left as they are.
+ * Every query counts, for good: of drafted tokens that may be rejected make the call when it is known which are, with the
+ * rejected rows of lse at -inf and before the lengths change.
  *   weights  [pages][cache heads][page_size] fp32, contiguous, 16-byte aligned: the places of the cache's pages.
  *   lse      [tokens][heads] fp32 as lilicorr_window_attention4 gives it for the same queries and keys, without a
  *            window; rows of -inf add nothing. 4-byte aligned.
