@@ -431,7 +431,7 @@ struct Shared4 {
   static constexpr int CPR = D / 32, P = W / 16;          // 16-byte pieces of a head, of a token
   static constexpr int RPI = kWave / P;                   // tokens that a copy moves
   static constexpr int KI = 32 / RPI;                     // copies of a tile's keys
-  static constexpr int SB = D == 64 && HB == 1 ? 4 : D / 32;  // bytes of a head's scales of a key, in LDS
+  static constexpr int SB = D / 32;                       // bytes of a head's scales of a key, in LDS
   static constexpr int SW = HB * SB;                      // and of the token's
   static constexpr bool kBoth = 32 * SW <= 128;           // one copy has keys' scales and values'
   static constexpr int SI = kBoth ? 1 : 32 * SW / 256;    // copies of the keys' scales
@@ -444,7 +444,7 @@ struct Shared4 {
   static constexpr int NS = C::NS;
   static constexpr uint32_t kBytes = NS * kStage;
   static_assert(C::kWaves == 4 && C::WK == 1, "four waves, the same keys");
-  static_assert(RPI <= 16 || RPI == 32, "a copy's tokens lie in one half, or are both");
+  static_assert(HB >= 2 && RPI <= 16, "heads to share, and a copy's tokens lie in one half");
 
   const unsigned char *k, *v, *ks, *vs;  // of the workgroup's first head
   lds_t lds;
@@ -493,11 +493,7 @@ struct Shared4 {
       const bool is_k = n < KI;
       const unsigned char* from = pick(is_k, k, v);
       const lds_t dst = to + n * 1024;
-      if constexpr (RPI == 32) {
-        copy16(dst, from + pick(lane_id() < 32, at.off0, at.off1) + c_off[i]);
-      } else {
-        copy16(dst, from + pick(n % KI < KI / 2, at.off0, at.off1), c_off[i]);
-      }
+      copy16(dst, from + pick(n % KI < KI / 2, at.off0, at.off1), c_off[i]);
     }
 #pragma unroll
     for (int i = 0; i < SCW; ++i) {
@@ -505,7 +501,7 @@ struct Shared4 {
       const lds_t dst = to + kS + n * 256;
       if constexpr (kBoth) {
         const int key = lane_id() % 32 * 4 / SW;
-        copy4<D == 64 && HB == 1>(dst, pick(VALUES && lane_id() >= 32, vs, ks) + pick(key < 16, at.off0, at.off1) / 16 + s_off[i]);
+        copy4<false>(dst, pick(VALUES && lane_id() >= 32, vs, ks) + pick(key < 16, at.off0, at.off1) / 16 + s_off[i]);
       } else {
         const int key = ((n % SI) * 64 + lane_id()) * 4 / SW;
         copy4<false>(dst, pick(n < SI, ks, vs) + pick(key < 16, at.off0, at.off1) / 16 + s_off[i]);
