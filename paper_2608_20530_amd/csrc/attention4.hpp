@@ -1096,12 +1096,13 @@ __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Arg
     constexpr int kBatch = FEW ? 64 / kAtOnce : 8;
     f32x4_t v[kBatch];
     auto load = [&](int b, uint64_t which) {
+      const float* at = a.part_o + ((s0 + b + lane / LPR) * a.rows + row) * a.d + x;
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         const int s = b + u * kAtOnce + lane / LPR;
         v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         if (s < here && x < a.d && (FEW || saw_of(which, b, u)))
-          v[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + ((s0 + s) * a.rows + row) * a.d + x);
+          v[u] = *reinterpret_cast<const f32x4_t*>(at + u * (kAtOnce * a.rows * a.d));
       }
     };
     f32x4_t ml = {-__builtin_inff(), 0.f, 0.f, 0.f};
@@ -1112,6 +1113,7 @@ __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Arg
     // the sum of a slot that saw nothing is 0; a NaN stays one
     const float f = ml[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[0] - grown);
     const bool saw = ml[1] != 0.f;
+    const float seen = saw ? f : -1.f;
     top = grown;
     l = l * f0 + wave_sum_dpp(saw ? f * ml[1] : 0.f);
     lu = lu * f0 + wave_sum_dpp(saw ? f * ml[2] : 0.f);
@@ -1122,10 +1124,9 @@ __global__ __launch_bounds__(kJoin4Threads) void attention4_join_kernel(Attn4Arg
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         const int s = b + u * kAtOnce + lane / LPR;
-        const bool on = s < here && saw_of(which, b, u);
-        const float w = __shfl(f, s & 63, kWave);
+        const float w = __shfl(seen, s & 63, kWave);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += on ? w * v[u][e] : 0.f;
+        for (int e = 0; e < 4; ++e) o[e] += w < 0.f ? 0.f : w * v[u][e];
       }
     }
   }
