@@ -633,7 +633,8 @@ lilicorr_status lilicorr_prefix_attention(const lilicorr_attention_args *args, h
  *
  * An element is E2M1 (a sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6), two to a byte, the even element in the low half. 32
  * neighbouring elements of a head are a block with a scale byte b, 1 to 252: they stand for their values times
- * 2^(b - 127). A block whose b is 255 is NaN throughout; 0, 253 and 254 are never written. Element x of head h of the
+ * 2^(b - 127). A block whose b is 255 is NaN throughout; 0, 253 and 254 are never written, and what a row that sees such a
+ * block gets has no meaning. Element x of head h of the
  * token at place o of page p lies at byte p * page_stride + o * token_stride + h * head_stride + x / 2 of k (keys) and of
  * v (values), its scale at a sixteenth of that offset (without x / 2) + x / 32 of k_scales and v_scales: scales are laid
  * out as codes are.
@@ -719,7 +720,8 @@ lilicorr_status lilicorr_window_attention4(const lilicorr_attention4_args *args,
  *   cache    v and v_scales are not read, and may be NULL.
  *   max_tokens, max_length   as for the attention: keys past max_length are left as they are, and so are requests with
  *            more than max_tokens queries.
- * In fp32 throughout. Each weight is added up by one wave in a fixed order, so the result is the same on every call. No two
+ * In fp32 throughout; a term is known to 2^-24 (d + 8) (1 + |lse| + scale sum |q k|) of it. Each weight is added up in a
+ * fixed order, by one wave or by four whose sums are added in theirs, so the result is the same on every call. No two
  * requests may share a page. decay finite and >= 0. Limits as for the attention.
  */
 typedef struct {

@@ -33,7 +33,8 @@ def quantise(x):
 
 
 def values(codes, scales):
-    """What codes [.., d / 2] and scales [.., d / 32] stand for, doubles [.., d]."""
+    """What codes [.., d / 2] and scales [.., d / 32] stand for, doubles [.., d]. 255 is NaN; 0, 253 and 254, which have no
+    meaning, are 2^-127 and NaN here."""
     n = np.stack((codes & 15, codes >> 4), -1).reshape(*codes.shape[:-1], -1)
     s = np.where(scales >= 253, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
     return np.where(n > 7, -1, 1) * VALUES[n & 7] * np.repeat(s, 32, -1)

@@ -646,10 +646,10 @@ __device__ __forceinline__ bool rows4(const Attn4Args& a, int tile, Rows4& r) {
 }
 
 // What bounds it, with 32 heads over 8 of 128: 256 tokens (100 to 16100 keys each) 445 us with the join, 5.1 TB/s: HBM, 0.76 of a
-// plain read. 64 blocks of 16 tokens 306 us, 8192 tokens of prefill 1930 (855 TFLOP/s, 0.64 of a library
+// plain read. 64 blocks of 16 tokens 308 us, 8192 tokens of prefill 1930 (855 TFLOP/s, 0.64 of a library
 // product): a tile of 32 rows and keys is 512 cycles of matrix instructions and 150 to 190 others, most of them
-// conversions, powers and sums, and two waves of a SIMD overlap a third of them. One token over 32768 keys 18.4 us:
-// latency, 14 of it here (lengths, pages, first tiles, output) and 5 in the join.
+// conversions, powers and sums, and two waves of a SIMD overlap a third of them. One token over 32768 keys 18.5 us:
+// latency, 14 of it here (lengths, pages, first tiles, output) and 4.6 in the join.
 template <typename C>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kSimdWaves, C::kSimdWaves)))
 void attention4_kernel(Attn4Args a) {

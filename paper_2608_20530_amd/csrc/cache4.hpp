@@ -1,8 +1,8 @@
 // The 4-bit paged cache: its elements, how the kernels convert them, the host's checks.
 //
 // An element is E2M1: a sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6, two to a byte, the even element low. 32 neighbouring
-// elements of a head share a byte b for the scale 2^(b - 127), and b of 253 to 255 says that the block is NaN
-// (the matrix cores' own block scale reads 255 so; 6 * 2^126 and 6 * 2^127 have no finite value).
+// elements of a head share a byte b for the scale 2^(b - 127), and b = 255 says that the block is NaN (the conversion reads
+// it so). 0, 253 and 254 are not written (6 * 2^126 and 6 * 2^127 are no bf16 values) and have no meaning.
 // Every other block's elements are bf16 values, so they go to the matrix cores without an error.
 #pragma once
 
